@@ -56,6 +56,7 @@ typedef enum rr_status {
 
 enum { RR_F32 = 0, RR_BF16 = 1 };             /* rr_config.dtype */
 enum { RR_ACT_GELU = 0, RR_ACT_SWIGLU = 1 };  /* rr_config.act   */
+enum { RR_ACT_NONE = 2 };                     /* rr_linear_config.act: one of these three */
 enum {                                        /* rr_config.flags */
   RR_INTRA_GPU      = 1u, /* Sec. 4.1: re-route every dropped token inside its own group          */
   RR_FILL_IN        = 2u, /* Sec. 4.2: fill padding slots with the best (k+1)-th-choice tokens     */
@@ -111,7 +112,7 @@ typedef struct rr_tables {
 
 /* Alignment: x, the expert weights, out, dout, w_router, logits and probs must be 16-byte aligned
  * (rows are moved with 16-byte vector instructions), every other array 4-byte aligned, the workspace
- * 256-byte aligned; a misaligned pointer is RR_ERR_INVALID_ARG (workspace: RR_ERR_WORKSPACE). */
+ * 256-byte aligned (rr_balance_loss*, rr_dropout* and rr_linear* state their own); a misaligned pointer is RR_ERR_INVALID_ARG (workspace: RR_ERR_WORKSPACE). */
 
 /* One-time, per-device host-side set-up for the current device: raises the dynamic-LDS limit of the
  * grouped-GEMM kernels and looks up the address of the static scratch buffer.  Idempotent and
@@ -198,6 +199,92 @@ int rr_moe_forward(const rr_config *cfg, const void *x, const float *w_router, c
 int rr_router_backward(const rr_config *cfg, const void *dout, const float *logits,
                        const rr_tables *tables, void *workspace, size_t workspace_bytes,
                        uint32_t grad_flags, float *dcombine_w, float *dlogits, void *stream);
+
+/* Load-balance loss of the router (the auxiliary loss of the paper's training recipe, Sec. 5.1) and per-expert counts.  With n
+ * the tokens that count, p_t the softmax of a token's scores over all experts (Eq. 5), c_e how often expert e is among the
+ * first k entries of a counted token's row of rank_expert (before capacity: what was chosen, not what was kept),
+ *     f_e = c_e / (k n),   P_e = (1/n) sum_t p_te,   loss = coef E sum_e f_e P_e     (coef if both are uniform).
+ *   logits      [T,E] fp32, as rr_router_scores and rr_moe_forward write them.  A score of -infinity is a probability of 0; a row
+ *               of nothing else has no probabilities at all
+ *   rank_expert [T,k+1] int32, as the same calls write it.  Entries outside [0, E) are counted for nobody
+ *   token_mask  [T] uint8 or NULL: 0 = the token does not count (padding); its scores and ranks may hold anything
+ *   coef        finite
+ *   loss        [1] fp32 out; 0 if no token counts
+ *   counts      [E+1] int32 out: c_e, then n
+ *   mean_prob   [E] fp32 out or NULL: P_e; 0 if no token counts
+ *   workspace   rr_balance_workspace_bytes(cfg); not the layer's own, which rr_router_backward still reads
+ * logits, rank_expert, loss, counts and mean_prob 4-byte aligned.  Of cfg T, E and k are used.  Sums over tokens are held in 64
+ * bits and added in a fixed order: results do not change from run to run. */
+int rr_balance_workspace_bytes(const rr_config *cfg, size_t *bytes);
+int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *rank_expert, const uint8_t *token_mask,
+                    float coef, float *loss, int32_t *counts, float *mean_prob,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradient of the router scores through P_e (the counts carry none):
+ *     dL/da_te = dloss coef E / n  p_te (f_e - sum_j f_j p_tj),   0 for a token that does not count.
+ *   counts      [E+1], as rr_balance_loss wrote them
+ *   dloss       [1] fp32 on the device, or NULL for 1
+ *   grad_flags  0, or RR_GRAD_ACCUMULATE: added to what dlogits holds (rr_router_backward's, say); rows of tokens that do not
+ *               count are then left as they are
+ *   dlogits     [T,E] fp32 in/out; not the same memory as logits */
+#define RR_GRAD_ACCUMULATE 2u
+int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const int32_t *counts, const uint8_t *token_mask,
+                             float coef, const float *dloss, uint32_t grad_flags, float *dlogits, void *stream);
+
+/* Dropout and the residual sum around a layer (Sec. 3: the row of a token that no expert processes is zero and its value rides
+ * the residual connection):
+ *     out_i = residual_i + (kept_i ? x_i s : 0),   kept_i = u_i >= m,   m = round(65536 p),   s = 65536 / (65536 - m).
+ * The mask is never stored: u_i is number i mod 8 of the eight 16-bit numbers (low half first, word by word) of the
+ * counter-based generator Philox4x32 with ten rounds (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", SC 2011)
+ * at counter (offset + i / 8) mod 2^64, key `seed`, so that the backward pass, or a program that holds only a part of the tensor
+ * (whole groups of 8), makes the same mask again.  A program advances `offset` by ceil(n / 8) per call.
+ *   n              elements, 1 .. 2^40
+ *   dtype          RR_F32 | RR_BF16, type of x, residual and out (dout and dx)
+ *   residual       [n] or NULL
+ *   p              0 <= p <= 1, taken in steps of 1 / 65536; at p = 1 out is the residual (or 0)
+ *   device_offset  NULL, or one uint64 on the device (8-byte aligned) that is added to `offset` when the kernel runs: a captured
+ *                  graph then draws another mask in each replay
+ *   out            [n]; may be x or residual itself
+ * A dropped element leaves nothing behind, whatever its value (NaN and infinities too).  The sum is made in fp32 and rounded
+ * once.  All data pointers 16-byte aligned. */
+int rr_dropout(int64_t n, int32_t dtype, const void *x, const void *residual, float p, uint64_t seed, uint64_t offset,
+               const uint64_t *device_offset, void *out, void *stream);
+/* dx_i = kept_i ? dout_i s : 0 with the mask of the forward call of the same p, seed and offset; dx may be dout itself.  (The
+ * gradient of the residual is dout.) */
+int rr_dropout_backward(int64_t n, int32_t dtype, const void *dout, float p, uint64_t seed, uint64_t offset,
+                        const uint64_t *device_offset, void *dx, void *stream);
+
+/* Dense projection, the matrix product of the dense FFN layers between the MoE layers (Sec. 5.1: every other FFN is one) and of
+ * experts that all tokens share:
+ *     z = x W^T + bias,   y = residual + act(z)
+ *     RR_ACT_NONE: act(z) = z;  RR_ACT_GELU: z Phi(z);  RR_ACT_SWIGLU: silu(z[:, :N]) * z[:, N:], W and z twice as wide.
+ * Rows R of W: N, or 2 N with RR_ACT_SWIGLU (the gate's rows, then the up projection's). */
+typedef struct rr_linear_config {
+  int32_t M;     /* rows (tokens), 1 .. 2^21                              */
+  int32_t K;     /* length of a row of x, a multiple of 8, up to 2^18     */
+  int32_t N;     /* columns of y, a multiple of 8, R up to 2^18           */
+  int32_t dtype; /* RR_F32 | RR_BF16: type of x, w, residual, y, pre and of their gradients; bias and dbias are fp32 */
+  int32_t act;   /* RR_ACT_NONE | RR_ACT_GELU | RR_ACT_SWIGLU             */
+} rr_linear_config;
+
+/* Scratch of rr_linear (backward = 0) or rr_linear_backward (1): a multiple of 256 bytes.  Host function. */
+int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, size_t *bytes);
+
+/*   x [M,K], w [R,K], bias [R] fp32 or NULL, residual [M,N] or NULL (may be y itself)
+ *   y   [M,N] out
+ *   pre [M,R] out or NULL: z, rounded to cfg->dtype, for rr_linear_backward
+ * Products are accumulated, and act and the sums made, in fp32; y is rounded once. */
+int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual,
+              void *y, void *pre, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Gradients for dy [M,N]: with dz = dy act'(z) (bf16: rounded to bf16 for the two products)
+ *     dx = dz W [M,K],   dw = dz^T x [R,K],   dbias = sum over rows of dz [R] fp32;   the residual's is dy.
+ *   pre     the forward call's; ignored with RR_ACT_NONE
+ *   dx, dw, dbias   each may be NULL (not all); x is needed for dw only and w for dx only, else NULL is allowed
+ * x, w, residual, y, pre, dy, dx and dw 16-byte aligned, bias and dbias 4-byte, the workspace 256-byte.  Sums run in a fixed
+ * order: results do not change from run to run. */
+int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w, const void *pre, const void *dy,
+                       void *dx, void *dw, float *dbias, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Per-kernel timing for benchmarks.  While enabled, every kernel the library launches is bracketed
  * by HIP events on the call's stream (events are created on first use and kept).  rr_profile_read

@@ -10,9 +10,9 @@ import os
 from dataclasses import dataclass
 
 RR_F32, RR_BF16 = 0, 1
-RR_ACT_GELU, RR_ACT_SWIGLU = 0, 1
+RR_ACT_GELU, RR_ACT_SWIGLU, RR_ACT_NONE = 0, 1, 2
 RR_INTRA_GPU, RR_FILL_IN, RR_POLICY_ARRIVAL, RR_QUOTA_PER_GROUP = 1, 2, 4, 8
-RR_GRAD_STRAIGHT_THROUGH = 1
+RR_GRAD_STRAIGHT_THROUGH, RR_GRAD_ACCUMULATE = 1, 2
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -26,6 +26,10 @@ class _Config(C.Structure):
     _fields_ = [("T", C.c_int32), ("d_model", C.c_int32), ("d_ff", C.c_int32), ("E", C.c_int32),
                 ("k", C.c_int32), ("G", C.c_int32), ("capacity_factor", C.c_float),
                 ("dtype", C.c_int32), ("act", C.c_int32), ("flags", C.c_uint32)]
+
+
+class _LinearConfig(C.Structure):
+    _fields_ = [("M", C.c_int32), ("K", C.c_int32), ("N", C.c_int32), ("dtype", C.c_int32), ("act", C.c_int32)]
 
 
 _TABLE_FIELDS = ("rank_expert", "slot", "slot_token", "fill_topk", "fill_total",
@@ -58,6 +62,23 @@ class RRConfig:
                        self.dtype, self.act, self.flags)
 
 
+@dataclass
+class RRLinearConfig:
+    M: int
+    K: int
+    N: int
+    dtype: int = RR_BF16
+    act: int = RR_ACT_NONE
+
+    @property
+    def rows(self) -> int:
+        """Rows of the weight matrix, columns of the pre-activations."""
+        return 2 * self.N if self.act == RR_ACT_SWIGLU else self.N
+
+    def c(self) -> _LinearConfig:
+        return _LinearConfig(self.M, self.K, self.N, self.dtype, self.act)
+
+
 def library_path() -> str:
     return os.path.join(_HERE, "librr.so")
 
@@ -88,6 +109,23 @@ def load_library():
     lib.rr_moe_forward.argtypes = [C.POINTER(_Config), vp, vp, vp, vp, vp, vp, vp, C.POINTER(_Tables), vp, vp, sz, vp]
     lib.rr_router_backward.restype = C.c_int
     lib.rr_router_backward.argtypes = [C.POINTER(_Config), vp, vp, C.POINTER(_Tables), vp, sz, C.c_uint32, vp, vp, vp]
+    f32, i64, u64, u32 = C.c_float, C.c_int64, C.c_uint64, C.c_uint32
+    lib.rr_balance_workspace_bytes.restype = C.c_int
+    lib.rr_balance_workspace_bytes.argtypes = [C.POINTER(_Config), C.POINTER(sz)]
+    lib.rr_balance_loss.restype = C.c_int
+    lib.rr_balance_loss.argtypes = [C.POINTER(_Config), vp, vp, vp, f32, vp, vp, vp, vp, sz, vp]
+    lib.rr_balance_loss_backward.restype = C.c_int
+    lib.rr_balance_loss_backward.argtypes = [C.POINTER(_Config), vp, vp, vp, f32, vp, u32, vp, vp]
+    lib.rr_dropout.restype = C.c_int
+    lib.rr_dropout.argtypes = [i64, i32, vp, vp, f32, u64, u64, vp, vp, vp]
+    lib.rr_dropout_backward.restype = C.c_int
+    lib.rr_dropout_backward.argtypes = [i64, i32, vp, f32, u64, u64, vp, vp, vp]
+    lib.rr_linear_workspace_bytes.restype = C.c_int
+    lib.rr_linear_workspace_bytes.argtypes = [C.POINTER(_LinearConfig), i32, C.POINTER(sz)]
+    lib.rr_linear.restype = C.c_int
+    lib.rr_linear.argtypes = [C.POINTER(_LinearConfig), vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.rr_linear_backward.restype = C.c_int
+    lib.rr_linear_backward.argtypes = [C.POINTER(_LinearConfig), vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.rr_init.restype = C.c_int
     lib.rr_init.argtypes = []
     lib.rr_profile_enable.restype = C.c_int
@@ -214,6 +252,132 @@ def rr_router_backward(cfg: RRConfig, dout, logits, tables: Tables | None, works
                                              C.byref(tc) if tc is not None else None, _ptr(workspace),
                                              workspace.numel(), RR_GRAD_STRAIGHT_THROUGH if straight_through else 0,
                                              _ptr(dcombine_w), _ptr(dlogits), _stream()), "rr_router_backward")
+
+
+def _size(t) -> int:
+    return 0 if t is None else t.numel()
+
+
+def _tensors(what: str, **checked):
+    """The operators around the layer: every tensor (or None) is dense, as large as the call takes it to be, of its type, and on
+    the current device, where the call is enqueued.  checked: name -> (tensor, elements, torch types)."""
+    import torch
+    for name, (t, numel, dtypes) in checked.items():
+        if t is None:
+            continue
+        if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+            raise RRError(f"{what}: {name} is on {t.device}, not on the current GPU")
+        if t.dtype not in dtypes or t.numel() != numel or not t.is_contiguous():
+            raise RRError(f"{what}: {name} must be dense, {numel} elements of {' or '.join(map(str, dtypes))}; "
+                          f"got {tuple(t.shape)} {t.dtype}")
+
+
+def _torch_type(dtype: int):
+    import torch
+    if dtype not in (RR_F32, RR_BF16):
+        raise RRError(f"unsupported dtype {dtype}")
+    return (torch.float32 if dtype == RR_F32 else torch.bfloat16,)
+
+
+def rr_balance_workspace_bytes(cfg: RRConfig) -> int:
+    n, cc = C.c_size_t(0), cfg.c()
+    _check(load_library().rr_balance_workspace_bytes(C.byref(cc), C.byref(n)), "rr_balance_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_balance_workspace(cfg: RRConfig, device="cuda"):
+    import torch
+    return torch.empty(rr_balance_workspace_bytes(cfg), dtype=torch.uint8, device=device)
+
+
+def rr_balance_loss(cfg: RRConfig, logits, rank_expert, coef: float, loss, counts, workspace, mean_prob=None, token_mask=None):
+    """loss [1], counts [E + 1] (int32: choices per expert, then the tokens that count), mean_prob [E] or None.
+    token_mask [T], uint8 or bool, or None: 0 = padding."""
+    import torch
+    f32, i32 = (torch.float32,), (torch.int32,)
+    _tensors("rr_balance_loss", logits=(logits, cfg.T * cfg.E, f32), rank_expert=(rank_expert, cfg.T * (cfg.k + 1), i32),
+             token_mask=(token_mask, cfg.T, (torch.uint8, torch.bool)), loss=(loss, 1, f32), counts=(counts, cfg.E + 1, i32),
+             mean_prob=(mean_prob, cfg.E, f32), workspace=(workspace, _size(workspace), (torch.uint8,)))
+    cc = cfg.c()
+    _check(load_library().rr_balance_loss(C.byref(cc), _ptr(logits), _ptr(rank_expert), _ptr(token_mask), coef, _ptr(loss),
+                                          _ptr(counts), _ptr(mean_prob), _ptr(workspace), _size(workspace), _stream()),
+           "rr_balance_loss")
+
+
+def rr_balance_loss_backward(cfg: RRConfig, logits, counts, coef: float, dlogits, dloss=None, token_mask=None,
+                             accumulate: bool = False):
+    """dlogits [T, E], written or (accumulate) added to; dloss [1] or None for 1."""
+    import torch
+    f32 = (torch.float32,)
+    _tensors("rr_balance_loss_backward", logits=(logits, cfg.T * cfg.E, f32), counts=(counts, cfg.E + 1, (torch.int32,)),
+             token_mask=(token_mask, cfg.T, (torch.uint8, torch.bool)), dloss=(dloss, 1, f32), dlogits=(dlogits, cfg.T * cfg.E, f32))
+    cc = cfg.c()
+    _check(load_library().rr_balance_loss_backward(C.byref(cc), _ptr(logits), _ptr(counts), _ptr(token_mask), coef, _ptr(dloss),
+                                                   RR_GRAD_ACCUMULATE if accumulate else 0, _ptr(dlogits), _stream()),
+           "rr_balance_loss_backward")
+
+
+def _dropout_type(x):
+    import torch
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise RRError(f"dropout: unsupported type {x.dtype}")
+    return RR_F32 if x.dtype == torch.float32 else RR_BF16
+
+
+def rr_dropout(x, p: float, seed: int, offset: int, out, residual=None, device_offset=None):
+    """out = residual + dropout(x), any shape; out may be x or residual.  device_offset: None or one int64 on the GPU, added to
+    `offset` when the kernel runs (captured graphs).  A call uses up (x.numel() + 7) // 8 counters from `offset` on."""
+    import torch
+    dtype, n = _dropout_type(x), x.numel()
+    _tensors("rr_dropout", x=(x, n, (x.dtype,)), residual=(residual, n, (x.dtype,)), out=(out, n, (x.dtype,)),
+             device_offset=(device_offset, 1, (torch.int64,)))
+    _check(load_library().rr_dropout(n, dtype, _ptr(x), _ptr(residual), p, seed, offset, _ptr(device_offset), _ptr(out), _stream()),
+           "rr_dropout")
+
+
+def rr_dropout_backward(dout, p: float, seed: int, offset: int, dx, device_offset=None):
+    """dx from dout with the mask of the forward call of the same p, seed and offset; dx may be dout."""
+    import torch
+    dtype, n = _dropout_type(dout), dout.numel()
+    _tensors("rr_dropout_backward", dout=(dout, n, (dout.dtype,)), dx=(dx, n, (dout.dtype,)),
+             device_offset=(device_offset, 1, (torch.int64,)))
+    _check(load_library().rr_dropout_backward(n, dtype, _ptr(dout), p, seed, offset, _ptr(device_offset), _ptr(dx), _stream()),
+           "rr_dropout_backward")
+
+
+def rr_linear_workspace_bytes(cfg: RRLinearConfig, backward: bool = False) -> int:
+    n, cc = C.c_size_t(0), cfg.c()
+    _check(load_library().rr_linear_workspace_bytes(C.byref(cc), 1 if backward else 0, C.byref(n)), "rr_linear_workspace_bytes")
+    return int(n.value)
+
+
+def alloc_linear_workspace(cfg: RRLinearConfig, backward: bool = False, device="cuda"):
+    import torch
+    return torch.empty(rr_linear_workspace_bytes(cfg, backward), dtype=torch.uint8, device=device)
+
+
+def rr_linear(cfg: RRLinearConfig, x, w, bias, residual, y, pre, workspace):
+    """y = residual + act(x W^T + bias); bias, residual and pre (the pre-activations, an output) may be None."""
+    import torch
+    t, f32 = _torch_type(cfg.dtype), (torch.float32,)
+    _tensors("rr_linear", x=(x, cfg.M * cfg.K, t), w=(w, cfg.rows * cfg.K, t), bias=(bias, cfg.rows, f32),
+             residual=(residual, cfg.M * cfg.N, t), y=(y, cfg.M * cfg.N, t), pre=(pre, cfg.M * cfg.rows, t),
+             workspace=(workspace, _size(workspace), (torch.uint8,)))
+    cc = cfg.c()
+    _check(load_library().rr_linear(C.byref(cc), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y), _ptr(pre), _ptr(workspace),
+                                    _size(workspace), _stream()), "rr_linear")
+
+
+def rr_linear_backward(cfg: RRLinearConfig, x, w, pre, dy, dx, dw, dbias, workspace):
+    """dx, dw and dbias (None: not wanted) from dy and the pre-activations of the forward call (None without an activation)."""
+    import torch
+    t, f32 = _torch_type(cfg.dtype), (torch.float32,)
+    _tensors("rr_linear_backward", x=(x, cfg.M * cfg.K, t), w=(w, cfg.rows * cfg.K, t), pre=(pre, cfg.M * cfg.rows, t),
+             dy=(dy, cfg.M * cfg.N, t), dx=(dx, cfg.M * cfg.K, t), dw=(dw, cfg.rows * cfg.K, t), dbias=(dbias, cfg.rows, f32),
+             workspace=(workspace, _size(workspace), (torch.uint8,)))
+    cc = cfg.c()
+    _check(load_library().rr_linear_backward(C.byref(cc), _ptr(x), _ptr(w), _ptr(pre), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(dbias),
+                                             _ptr(workspace), _size(workspace), _stream()), "rr_linear_backward")
 
 
 def rr_profile_enable(on: bool):

@@ -45,7 +45,8 @@ static hipEvent_t g_open[K_COUNT];
 static const char *const g_kernel_names[K_COUNT] = {
     "router_scores", "topk_rank", "scan_candidates", "scatter_candidates", "select_slot",
     "ir_count", "ir_scan", "ir_weights", "dispatch_gather", "ffn_gate_up", "ffn_down", "combine",
-    "router_backward", "route_small"};
+    "router_backward", "route_small", "balance_loss", "balance_loss_backward", "dropout", "dropout_backward", "linear",
+    "linear_backward"};
 
 static hipEvent_t get_event() {
   if (!g_free_events.empty()) {
@@ -381,6 +382,108 @@ int rr_router_backward(const rr_config *cfg, const void *dout, const float *logi
   const float *lg = logits ? logits : W.logits;
   hipError_t e = launch_router_backward(D, dout, lg, tb, W, (grad_flags & RR_GRAD_STRAIGHT_THROUGH) != 0, dcombine_w,
                                         dlogits, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? RR_OK : RR_ERR_HIP;
+}
+
+int rr_balance_workspace_bytes(const rr_config *cfg, size_t *bytes) {
+  if (!bytes) return RR_ERR_INVALID_ARG;
+  Dims D;
+  const int rc = make_dims(cfg, false, &D);
+  if (rc == RR_OK) *bytes = balance_workspace();
+  return rc;
+}
+
+int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *rank_expert, const uint8_t *token_mask, float coef,
+                    float *loss, int32_t *counts, float *mean_prob, void *workspace, size_t workspace_bytes, void *stream) {
+  Dims D;
+  const int rc = make_dims(cfg, false, &D);
+  if (rc != RR_OK) return rc;
+  if (!logits || !rank_expert || !loss || !counts || !isfinite(coef)) return RR_ERR_INVALID_ARG;
+  if (!aligned4(logits) || !aligned4(rank_expert) || !aligned4(loss) || !aligned4(counts) || !aligned4(mean_prob))
+    return RR_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < balance_workspace()) return RR_ERR_WORKSPACE;
+  const hipError_t e = launch_balance_loss(D.T, D.E, D.k, logits, rank_expert, token_mask, coef, loss, counts, mean_prob, workspace,
+                                           static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? RR_OK : RR_ERR_HIP;
+}
+
+int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const int32_t *counts, const uint8_t *token_mask, float coef,
+                             const float *dloss, uint32_t grad_flags, float *dlogits, void *stream) {
+  Dims D;
+  const int rc = make_dims(cfg, false, &D);
+  if (rc != RR_OK) return rc;
+  if (!logits || !counts || !dlogits || logits == dlogits || !isfinite(coef)) return RR_ERR_INVALID_ARG;
+  if (grad_flags & ~(uint32_t)RR_GRAD_ACCUMULATE) return RR_ERR_INVALID_ARG;
+  if (!aligned4(logits) || !aligned4(counts) || !aligned4(dloss) || !aligned4(dlogits)) return RR_ERR_INVALID_ARG;
+  const hipError_t e = launch_balance_grad(D.T, D.E, D.k, logits, counts, token_mask, coef, dloss,
+                                           (grad_flags & RR_GRAD_ACCUMULATE) != 0, dlogits, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? RR_OK : RR_ERR_HIP;
+}
+
+static int dropout(int64_t n, int32_t dtype, const void *x, const void *residual, float p, uint64_t seed, uint64_t offset,
+                   const uint64_t *device_offset, void *out, KernelId id, void *stream) {
+  if (n <= 0 || !x || !out || !(p >= 0.0f) || p > 1.0f) return RR_ERR_INVALID_ARG;
+  if ((dtype != RR_F32 && dtype != RR_BF16) || n > (int64_t)1 << 40) return RR_ERR_UNSUPPORTED;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(out) || (reinterpret_cast<uintptr_t>(device_offset) & 7))
+    return RR_ERR_INVALID_ARG;
+  const u32 m = (u32)floor(65536.0 * (double)p + 0.5);
+  const hipError_t e = launch_dropout(n, dtype, x, residual, m, seed, offset, reinterpret_cast<const unsigned long long *>(device_offset),
+                                      out, id, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? RR_OK : RR_ERR_HIP;
+}
+
+int rr_dropout(int64_t n, int32_t dtype, const void *x, const void *residual, float p, uint64_t seed, uint64_t offset,
+               const uint64_t *device_offset, void *out, void *stream) {
+  return dropout(n, dtype, x, residual, p, seed, offset, device_offset, out, K_DROPOUT, stream);
+}
+
+int rr_dropout_backward(int64_t n, int32_t dtype, const void *dout, float p, uint64_t seed, uint64_t offset,
+                        const uint64_t *device_offset, void *dx, void *stream) {
+  return dropout(n, dtype, dout, nullptr, p, seed, offset, device_offset, dx, K_DROPOUT_BWD, stream);
+}
+
+static int check_linear(const rr_linear_config *c) {
+  if (!c || c->M <= 0 || c->K <= 0 || c->N <= 0) return RR_ERR_INVALID_ARG;
+  if (c->dtype != RR_F32 && c->dtype != RR_BF16) return RR_ERR_UNSUPPORTED;
+  if (c->act != RR_ACT_NONE && c->act != RR_ACT_GELU && c->act != RR_ACT_SWIGLU) return RR_ERR_UNSUPPORTED;
+  constexpr int32_t kMaxRows = 1 << 21, kMaxWidth = 1 << 18;
+  if (c->K % 8 || c->N % 8 || c->M > kMaxRows || c->K > kMaxWidth || c->N > kMaxWidth / (c->act == RR_ACT_SWIGLU ? 2 : 1))
+    return RR_ERR_UNSUPPORTED;
+  return RR_OK;
+}
+
+int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, size_t *bytes) {
+  if (!bytes || (backward != 0 && backward != 1)) return RR_ERR_INVALID_ARG;
+  const int rc = check_linear(cfg);
+  if (rc == RR_OK) *bytes = linear_workspace(*cfg, backward != 0);
+  return rc;
+}
+
+int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual, void *y, void *pre,
+              void *workspace, size_t workspace_bytes, void *stream) {
+  const int rc = check_linear(cfg);
+  if (rc != RR_OK) return rc;
+  if (!x || !w || !y) return RR_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w) || !aligned4(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre))
+    return RR_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < linear_workspace(*cfg, false))
+    return RR_ERR_WORKSPACE;
+  if (device_setup() < 0) return RR_ERR_HIP;
+  const hipError_t e = launch_linear(*cfg, x, w, bias, residual, y, pre, workspace, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? RR_OK : RR_ERR_HIP;
+}
+
+int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w, const void *pre, const void *dy, void *dx, void *dw,
+                       float *dbias, void *workspace, size_t workspace_bytes, void *stream) {
+  const int rc = check_linear(cfg);
+  if (rc != RR_OK) return rc;
+  if (!dy || (!dx && !dw && !dbias) || (dx && !w) || (dw && !x) || (cfg->act != RR_ACT_NONE && !pre)) return RR_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(w) || !aligned16(pre) || !aligned16(dy) || !aligned16(dx) || !aligned16(dw) || !aligned4(dbias))
+    return RR_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < linear_workspace(*cfg, true))
+    return RR_ERR_WORKSPACE;
+  if (device_setup() < 0) return RR_ERR_HIP;
+  const hipError_t e = launch_linear_backward(*cfg, x, w, pre, dy, dx, dw, dbias, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? RR_OK : RR_ERR_HIP;
 }
 

@@ -1,0 +1,300 @@
+// Load-balance loss of the router, per-expert counts, and the gradient of the scores:
+//   f_e = c_e / (k n),  P_e = (1/n) sum_t p_te,  loss = coef E sum_e f_e P_e,
+//   dL/da_te = dloss coef E / n  p_te (f_e - sum_j f_j p_tj),   p_t = softmax(a_t) over all experts, n counted tokens.
+//
+// LANES lanes share a token's row, four experts each, so that a wave reads 64 / LANES rows at once; maximum and sum go over
+// those lanes by shuffles.  A lane sums its four experts' probabilities over its rows in 64 bits and never touches memory
+// for them; one record per workgroup (sums, counts, n) is added up in a fixed order by balance_finish, or by the workgroup
+// itself where there is only one.  The gradient needs f, so it is a second pass over the scores: the probabilities are made
+// again rather than stored.
+#include "rr_device.h"
+
+namespace rr {
+
+namespace {
+
+constexpr int BL_THREADS = 256;
+constexpr int BL_MAX_BLOCKS = 1024;  // records that balance_finish adds up
+
+// What a workgroup leaves: probabilities summed, choices and tokens counted.
+struct BalanceRecord {
+  double prob[kMaxE];
+  int32_t count[kMaxE];
+  int32_t tokens, pad[31];
+};
+
+struct BalanceArgs {
+  const float *logits;
+  const int32_t *rank_expert;
+  const uint8_t *mask;
+  int T, E, k;
+  float coef;
+  float *loss;
+  int32_t *counts;
+  float *mean_prob;
+  BalanceRecord *records;
+};
+
+// The four experts of a lane: in a row (VEC: the row is read 16 bytes at a time) or LANES apart.
+template <int LANES, bool VEC>
+__device__ inline int expert_of(int lane, int j) {
+  return VEC ? 4 * (lane & (LANES - 1)) + j : (lane & (LANES - 1)) + LANES * j;
+}
+template <int LANES, bool VEC>
+__device__ inline void load_row(const float *row, int E, int lane, float (&a)[4]) {
+  if (VEC) {
+    const int e = expert_of<LANES, VEC>(lane, 0);
+    const float4 v = e < E ? *reinterpret_cast<const float4 *>(row + e) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    a[0] = v.x; a[1] = v.y; a[2] = v.z; a[3] = v.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int e = expert_of<LANES, VEC>(lane, j);
+      a[j] = e < E ? row[e] : -INFINITY;
+    }
+  }
+}
+template <int LANES>
+__device__ inline float row_max(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+template <int LANES>
+__device__ inline float row_sum(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+// Scores -> unnormalised probabilities; returns 1 / their sum (0 for a row of -infinity only).
+template <int LANES>
+__device__ inline float softmax_row(float (&a)[4]) {
+  const float m = row_max<LANES>(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
+  const float top = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a[j] = expf(a[j] - top);
+  const float sum = row_sum<LANES>(a[0] + a[1] + a[2] + a[3]);
+  return sum == 0.0f ? 0.0f : 1.0f / sum;
+}
+
+// One thread per expert, the first wave: loss and the outputs from the sums.
+__device__ inline void write_balance(const BalanceArgs &A, double prob, int count, int tokens) {
+  const int e = threadIdx.x;
+  double term = 0.0;
+  if (e < A.E) {
+    const double mean = tokens > 0 ? prob / tokens : 0.0;
+    term = tokens > 0 ? (double)count / ((double)A.k * tokens) * mean : 0.0;
+    A.counts[e] = count;
+    if (A.mean_prob) A.mean_prob[e] = (float)mean;
+  }
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) term += __shfl_xor(term, o);
+  if (e == 0) {
+    A.loss[0] = (float)((double)A.coef * A.E * term);
+    A.counts[A.E] = tokens;
+  }
+}
+
+template <int LANES, bool VEC>
+__global__ __launch_bounds__(BL_THREADS) void balance_loss_kernel(BalanceArgs A) {
+  constexpr int ROWS = kWave / LANES, WAVES = BL_THREADS / kWave;
+  __shared__ double sums[WAVES][kMaxE];
+  __shared__ int32_t hist[kMaxE];
+  __shared__ int32_t live_tokens;
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid >> 6, E = A.E, k = A.k;
+  if (tid < kMaxE) hist[tid] = 0;
+  if (tid == 0) live_tokens = 0;
+  __syncthreads();
+  double prob[4] = {0.0, 0.0, 0.0, 0.0};
+  int live = 0;
+  const int step = gridDim.x * WAVES * ROWS;
+  for (int t0 = (blockIdx.x * WAVES + w) * ROWS; t0 < A.T; t0 += step) {
+    const int t = t0 + lane / LANES;
+    const bool counted = t < A.T && (!A.mask || A.mask[t]);
+    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (counted) load_row<LANES, VEC>(A.logits + (size_t)t * E, E, lane, a);
+    const float inv = softmax_row<LANES>(a);
+    if (counted) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) prob[j] += (double)(a[j] * inv);
+      if ((lane & (LANES - 1)) == 0) {
+        ++live;
+        for (int r = 0; r < k; ++r) {
+          const int e = A.rank_expert[(size_t)t * (k + 1) + r];
+          if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int o = kWave / 2; o >= LANES; o >>= 1)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) prob[j] += __shfl_xor(prob[j], o);
+  if (lane < LANES)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (expert_of<LANES, VEC>(lane, j) < kMaxE) sums[w][expert_of<LANES, VEC>(lane, j)] = prob[j];
+  if (live) atomicAdd(&live_tokens, live);
+  __syncthreads();
+  if (tid >= kWave) return;
+  double total = 0.0;
+  if (tid < E)
+#pragma unroll
+    for (int q = 0; q < WAVES; ++q) total += sums[q][tid];
+  if (gridDim.x == 1) {
+    write_balance(A, total, hist[tid], live_tokens);
+    return;
+  }
+  BalanceRecord &R = A.records[blockIdx.x];
+  R.prob[tid] = total;
+  R.count[tid] = hist[tid];
+  if (tid == 0) R.tokens = live_tokens;
+}
+
+// Adds up the records: thread (part, expert) every 16th record, then the parts in order.
+__global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs A, int n) {
+  constexpr int PARTS = 1024 / kWave;
+  __shared__ double sums[PARTS][kMaxE];
+  __shared__ int32_t hist[PARTS][kMaxE], tokens[PARTS];
+  const int e = threadIdx.x & (kWave - 1), part = threadIdx.x >> 6;
+  double prob = 0.0;
+  int count = 0, live = 0;
+  for (int i = part; i < n; i += PARTS) {
+    prob += A.records[i].prob[e];
+    count += A.records[i].count[e];
+    live += A.records[i].tokens;
+  }
+  sums[part][e] = prob;
+  hist[part][e] = count;
+  if (e == 0) tokens[part] = live;
+  __syncthreads();
+  if (part > 0) return;
+  prob = 0.0;
+  count = live = 0;
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q) {
+    prob += sums[q][e];
+    count += hist[q][e];
+    live += tokens[q];
+  }
+  write_balance(A, prob, count, live);
+}
+
+// A sum that is not fused with the product before it: accumulating adds the very numbers that the call writes otherwise.
+__device__ inline float add(float a, float b) {
+#pragma clang fp contract(off)
+  return a + b;
+}
+
+struct BalanceGradArgs {
+  const float *logits;
+  const int32_t *counts;
+  const uint8_t *mask;
+  int T, E, k;
+  float coef;
+  const float *dloss;
+  float *dlogits;
+};
+
+template <int LANES, bool VEC, bool ADD>
+__global__ __launch_bounds__(BL_THREADS) void balance_grad_kernel(BalanceGradArgs A) {
+  constexpr int ROWS = kWave / LANES, WAVES = BL_THREADS / kWave;
+  const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x >> 6, E = A.E;
+  const int n = A.counts[E];
+  const float each = n > 0 ? 1.0f / ((float)A.k * (float)n) : 0.0f;
+  const float scale = n > 0 ? (A.dloss ? *A.dloss : 1.0f) * A.coef * (float)E / (float)n : 0.0f;
+  float f[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int e = expert_of<LANES, VEC>(lane, j);
+    f[j] = e < E ? (float)A.counts[e] * each : 0.0f;
+  }
+  const int step = gridDim.x * WAVES * ROWS;
+  for (int t0 = (blockIdx.x * WAVES + w) * ROWS; t0 < A.T; t0 += step) {
+    const int t = t0 + lane / LANES;
+    const bool in = t < A.T, counted = in && (!A.mask || A.mask[t]);
+    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (counted) load_row<LANES, VEC>(A.logits + (size_t)t * E, E, lane, a);
+    const float inv = softmax_row<LANES>(a);
+    const float mean = row_sum<LANES>(f[0] * a[0] + f[1] * a[1] + f[2] * a[2] + f[3] * a[3]) * inv;
+    if (ADD ? !counted : !in) continue;
+    float *row = A.dlogits + (size_t)t * E;
+    float g[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = counted ? scale * (a[j] * inv) * (f[j] - mean) : 0.0f;
+    if (VEC) {
+      const int e = expert_of<LANES, VEC>(lane, 0);
+      if (e < E) {
+        float4 *at = reinterpret_cast<float4 *>(row + e);
+        const float4 v = ADD ? *at : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (ADD) *at = make_float4(add(v.x, g[0]), add(v.y, g[1]), add(v.z, g[2]), add(v.w, g[3]));
+        else *at = make_float4(g[0], g[1], g[2], g[3]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = expert_of<LANES, VEC>(lane, j);
+        if (e < E) row[e] = ADD ? add(row[e], g[j]) : g[j];
+      }
+    }
+  }
+}
+
+// Workgroups for T rows, ROWS a wave.
+int balance_blocks(int T, int lanes, int most) {
+  const int rows = kWave / lanes * (BL_THREADS / kWave);
+  const int blocks = (T + rows - 1) / rows;
+  return blocks < most ? blocks : most;
+}
+
+bool aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+template <class F>
+void with_lanes(int E, bool vec, F f) {
+  auto pick = [&](auto v) {
+    constexpr bool VEC = decltype(v)::value;
+    if (E <= 4) f(std::integral_constant<int, 1>{}, std::integral_constant<bool, VEC>{});
+    else if (E <= 8) f(std::integral_constant<int, 2>{}, std::integral_constant<bool, VEC>{});
+    else if (E <= 16) f(std::integral_constant<int, 4>{}, std::integral_constant<bool, VEC>{});
+    else if (E <= 32) f(std::integral_constant<int, 8>{}, std::integral_constant<bool, VEC>{});
+    else f(std::integral_constant<int, 16>{}, std::integral_constant<bool, VEC>{});
+  };
+  if (vec) pick(std::true_type{});
+  else pick(std::false_type{});
+}
+
+}  // namespace
+
+size_t balance_workspace() { return sizeof(BalanceRecord) * BL_MAX_BLOCKS; }
+
+hipError_t launch_balance_loss(int T, int E, int k, const float *logits, const int32_t *rank_expert, const uint8_t *mask, float coef,
+                               float *loss, int32_t *counts, float *mean_prob, void *ws, hipStream_t s) {
+  const BalanceArgs A{logits, rank_expert, mask, T, E, k, coef, loss, counts, mean_prob, static_cast<BalanceRecord *>(ws)};
+  int blocks = 1;
+  prof_begin(K_BALANCE, s);
+  with_lanes(E, E % 4 == 0 && aligned(logits), [&](auto lanes, auto vec) {
+    constexpr int LANES = decltype(lanes)::value;
+    blocks = balance_blocks(T, LANES, BL_MAX_BLOCKS);
+    balance_loss_kernel<LANES, decltype(vec)::value><<<blocks, BL_THREADS, 0, s>>>(A);
+  });
+  if (blocks > 1) balance_finish_kernel<<<1, 1024, 0, s>>>(A, blocks);
+  prof_end(K_BALANCE, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_balance_grad(int T, int E, int k, const float *logits, const int32_t *counts, const uint8_t *mask, float coef,
+                               const float *dloss, bool add, float *dlogits, hipStream_t s) {
+  const BalanceGradArgs A{logits, counts, mask, T, E, k, coef, dloss, dlogits};
+  prof_begin(K_BALANCE_BWD, s);
+  with_lanes(E, E % 4 == 0 && aligned(logits) && aligned(dlogits), [&](auto lanes, auto vec) {
+    constexpr int LANES = decltype(lanes)::value;
+    constexpr bool VEC = decltype(vec)::value;
+    const int blocks = balance_blocks(T, LANES, 1 << 14);
+    if (add) balance_grad_kernel<LANES, VEC, true><<<blocks, BL_THREADS, 0, s>>>(A);
+    else balance_grad_kernel<LANES, VEC, false><<<blocks, BL_THREADS, 0, s>>>(A);
+  });
+  prof_end(K_BALANCE_BWD, s);
+  return hipGetLastError();
+}
+
+}  // namespace rr

@@ -84,5 +84,33 @@ __device__ inline int xcd_block(int g, int NB) {
   return g < main ? (g & 7) * per + (g >> 3) : g;
 }
 
+// Four words of random bits: Philox4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as
+// 1, 2, 3", SC 2011) at counter words (low, high, 0, 0) with the two words of `seed` as key.
+__device__ inline void philox4x32_10(unsigned long long counter, unsigned long long seed, u32 (&out)[4]) {
+  u32 c0 = (u32)counter, c1 = (u32)(counter >> 32), c2 = 0u, c3 = 0u, k0 = (u32)seed, k1 = (u32)(seed >> 32);
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
+    c0 = (u32)(b >> 32) ^ c1 ^ k0;
+    c1 = (u32)b;
+    c2 = (u32)(a >> 32) ^ c3 ^ k1;
+    c3 = (u32)a;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  out[0] = c0; out[1] = c1; out[2] = c2; out[3] = c3;
+}
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+// two fp32 -> packed bf16 pair, round to nearest even (v_cvt_pk_bf16_f32), first value in the low half
+__device__ inline u32 pack_bf16(float a, float b) {
+  const f32x2_t f = {a, b};
+  return __builtin_bit_cast(u32, __builtin_convertvector(f, bf16x2_t));
+}
+
+// g Phi(g).  (A single polynomial for erfc in 1 / (1 + 0.45 |g|) is 3 us less of a 6161 x 2728 up projection, 55 us, but
+// 5 times the error for |g| < 1: 41 of 2^20 normal arguments of sigma 0.3 round to another bf16 than g Phi(g) does, here 3.)
+__device__ inline float gelu_erf(float g) { return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f)); }
 
 }  // namespace rr

@@ -78,16 +78,6 @@ __device__ inline float silu(float g) { return g / (1.0f + __expf(-g)); }
 // 5632, 16 experts, 128 x 128 tiles: the layer 235 us, with the division 237.
 __device__ inline float silu_fast(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-// two fp32 -> packed bf16 pair, round to nearest even (v_cvt_pk_bf16_f32), first value in the low half
-__device__ inline u32 pack_bf16(float a, float b) {
-  const f32x2_t f = {a, b};
-  return __builtin_bit_cast(u32, __builtin_convertvector(f, bf16x2_t));
-}
-// g Phi(g).  (A single polynomial for erfc in 1 / (1 + 0.45 |g|) is 3 us less of a 6161 x 2728 up projection, 55 us, but
-// 5 times the error for |g| < 1: 41 of 2^20 normal arguments of sigma 0.3 round to another bf16 than g Phi(g) does, here 3.)
-__device__ inline float gelu_erf(float g) { return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f)); }
 constexpr int GB_BK = 64;             // bf16 elements per K chunk = 128 B per LDS row
 constexpr int GB_ROW_BYTES = 128;
 [[maybe_unused]] constexpr u32 BUF_FLAGS = 0x00020000; // raw buffer descriptor word 3 (32-bit data format)

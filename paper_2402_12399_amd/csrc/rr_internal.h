@@ -105,6 +105,7 @@ struct Launch {
 enum KernelId {
   K_ROUTER = 0, K_TOPK, K_SCAN_CAND, K_SCATTER_CAND, K_SELECT_SLOT,
   K_IR_COUNT, K_IR_SCAN, K_IR_WEIGHTS, K_GATHER, K_FFN_UP, K_FFN_DOWN, K_COMBINE, K_ROUTER_BWD, K_ROUTE_SMALL,
+  K_BALANCE, K_BALANCE_BWD, K_DROPOUT, K_DROPOUT_BWD, K_LINEAR, K_LINEAR_BWD,
   K_COUNT
 };
 
@@ -160,5 +161,20 @@ hipError_t launch_combine(const Dims &D, const rr_tables &tb, const Work &W, voi
 hipError_t launch_router_backward(const Dims &D, const void *dout, const float *logits, const rr_tables &tb,
                                   const Work &W, bool straight_through, float *dcombine_w, float *dlogits,
                                   hipStream_t s);
+
+// The operators around the layer: arguments as in rr.h, validated by their entry points.
+size_t balance_workspace();
+hipError_t launch_balance_loss(int T, int E, int k, const float *logits, const int32_t *rank_expert, const uint8_t *mask, float coef,
+                               float *loss, int32_t *counts, float *mean_prob, void *ws, hipStream_t s);
+hipError_t launch_balance_grad(int T, int E, int k, const float *logits, const int32_t *counts, const uint8_t *mask, float coef,
+                               const float *dloss, bool add, float *dlogits, hipStream_t s);
+// m of 65536: random numbers below it drop their element
+hipError_t launch_dropout(long long n, int dtype, const void *x, const void *residual, u32 m, unsigned long long seed,
+                          unsigned long long offset, const unsigned long long *device_offset, void *out, KernelId id, hipStream_t s);
+size_t linear_workspace(const rr_linear_config &c, bool backward);
+hipError_t launch_linear(const rr_linear_config &c, const void *x, const void *w, const float *bias, const void *residual, void *y,
+                         void *pre, void *ws, hipStream_t s);
+hipError_t launch_linear_backward(const rr_linear_config &c, const void *x, const void *w, const void *pre, const void *dy, void *dx,
+                                  void *dw, float *dbias, void *ws, hipStream_t s);
 
 }  // namespace rr

@@ -44,14 +44,6 @@ union Frag {
   bf16x8 v;
 };
 
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-
-// two fp32 -> packed bf16 pair, round to nearest even (v_cvt_pk_bf16_f32), element 0 in the low half
-__device__ inline u32 pack_bf16(float a, float b) {
-  const f32x2_t f = {a, b};
-  return __builtin_bit_cast(u32, __builtin_convertvector(f, bf16x2_t));
-}
 __device__ inline float lo_half(u32 p) { return __builtin_bit_cast(float, p << 16); }
 __device__ inline float hi_half(u32 p) { return __builtin_bit_cast(float, p & 0xffff0000u); }
 

@@ -1,0 +1,212 @@
+"""CPU checks of the operators around the layer: what the plain implementations of the tests rest on, and every refusal - nothing
+here reaches a kernel launch."""
+import ctypes as C
+import math
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_12399_amd as rr
+from paper_2402_12399_amd import binding
+from tests import operators_ref as ref
+
+INVALID, UNSUPPORTED, WORKSPACE = -1, -2, -3
+FAKE, ODD16, ODD4 = C.c_void_p(0x1000), C.c_void_p(0x1008), C.c_void_p(0x1002)
+BIG = 1 << 50
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(rr.library_path()):
+        from paper_2402_12399_amd import build
+        build.build(verbose=False)
+    return rr.load_library()
+
+
+# ------------------------------------------------------------------ the plain implementations
+
+@pytest.mark.parametrize("low,high,key,want", [
+    # the published known answers of Philox4x32-10
+    (0, 0, 0, (0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8)),
+    (2 ** 64 - 1, 2 ** 64 - 1, 2 ** 64 - 1, (0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD)),
+    (0x85A308D3243F6A88, 0x0370734413198A2E, 0x299F31D0A4093822, (0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1)),
+])
+def test_generator_known_answers(low, high, key, want):
+    assert tuple(int(v) for v in ref.philox4x32([low], key, high)[0]) == want
+
+
+def test_generator_is_uniform_and_counters_wrap():
+    u = ref.random_halves(12345, 7, 1 << 20)
+    # a mean of 2^20 uniform numbers: sigma 65536 / sqrt(12 * 2^20) = 18.5
+    assert abs(u.astype(np.float64).mean() - 32767.5) < 6 * 18.5
+    assert np.array_equal(u[8:24], ref.random_halves(12345, 8, 16))
+    assert np.array_equal(ref.random_halves(5, 2 ** 64 - 1, 16)[8:], ref.random_halves(5, 0, 8))
+
+
+@pytest.mark.parametrize("name", ["none", "gelu", "swiglu"])
+def test_plain_linear_gradients_against_differences(name):
+    g = torch.Generator().manual_seed(3)
+    R = 12 if name == "swiglu" else 6
+    x, w = torch.randn(5, 4, generator=g).double(), torch.randn(R, 4, generator=g).double()
+    b, dy = torch.randn(R, generator=g).double(), torch.randn(5, 6, generator=g).double()
+    loss = lambda x, w, b: float((ref.linear(x, w, b, None, name)[0] * dy).sum())
+    got = ref.linear_backward(x, w, ref.linear(x, w, b, None, name)[1], dy, name)
+    h = 1e-6
+    for which, t, grad in ((0, x, got["dx"]), (1, w, got["dw"]), (2, b, got["dbias"])):
+        for i in range(t.numel()):
+            args = [x.clone(), w.clone(), b.clone()]
+            args[which].view(-1)[i] += h
+            up = loss(*args)
+            args[which].view(-1)[i] -= 2 * h
+            assert abs((up - loss(*args)) / (2 * h) - float(grad.reshape(-1)[i])) < 1e-7 * (1 + abs(float(grad.reshape(-1)[i]))) + 1e-8
+
+
+def test_plain_balance_gradient_against_differences():
+    g = torch.Generator().manual_seed(4)
+    a = torch.randn(7, 5, generator=g).double()
+    ranks = torch.argsort(-a, dim=1)[:, :3].int()
+    mask = torch.tensor([1, 1, 0, 1, 1, 1, 0])
+    got = ref.balance(a, ranks, 2, 0.3, mask)
+    h = 1e-6
+    for t in range(7):
+        for e in range(5):
+            up, dn = a.clone(), a.clone()
+            up[t, e] += h
+            dn[t, e] -= h
+            d = (ref.balance(up, ranks, 2, 0.3, mask)["loss"] - ref.balance(dn, ranks, 2, 0.3, mask)["loss"]) / (2 * h)
+            assert abs(float(d - got["dlogits"][t, e])) < 1e-8
+    # uniform routing: the loss is the coefficient
+    u = ref.balance(torch.zeros(4, 4), torch.tensor([[0, 1, 2], [1, 2, 3], [2, 3, 0], [3, 0, 1]]), 2, 0.3)
+    assert math.isclose(float(u["loss"]), 0.3, rel_tol=1e-12)
+
+
+def test_plain_dropout_expectation():
+    x = torch.ones(1 << 18)
+    out, keep, scale = ref.dropout(x, None, 0.1, 99, 0)
+    # sigma of the mean: sqrt(p / (1 - p) / n)
+    assert abs(float(out.mean()) - 1.0) < 6 * math.sqrt(0.1 / 0.9 / x.numel())
+    assert set(out[keep].tolist()) == {scale} and not out[~keep].any()
+
+
+# ------------------------------------------------------------------ refusals at the C entries
+
+def _linear(**kw):
+    c = dict(M=16, K=64, N=64, dtype=rr.RR_BF16, act=rr.RR_ACT_GELU)
+    c.update(kw)
+    return rr.RRLinearConfig(**c).c()
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(), 0), (dict(M=1, K=8, N=8), 0), (dict(M=0), INVALID), (dict(K=0), INVALID), (dict(N=-8), INVALID),
+    (dict(K=60), UNSUPPORTED), (dict(N=4), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(act=3), UNSUPPORTED), (dict(act=-1), UNSUPPORTED),
+    (dict(M=1 << 21), 0), (dict(M=(1 << 21) + 1), UNSUPPORTED), (dict(K=1 << 18), 0), (dict(K=(1 << 18) + 8), UNSUPPORTED),
+    (dict(N=1 << 18), 0), (dict(N=(1 << 18) + 8), UNSUPPORTED), (dict(N=1 << 18, act=rr.RR_ACT_SWIGLU), UNSUPPORTED),
+    (dict(N=1 << 17, act=rr.RR_ACT_SWIGLU), 0),
+])
+def test_linear_configurations(lib, kw, want):
+    n, c = C.c_size_t(0), _linear(**kw)
+    for backward in (0, 1):
+        assert lib.rr_linear_workspace_bytes(C.byref(c), backward, C.byref(n)) == want
+        if want == 0:
+            assert n.value % 256 == 0
+    if want:
+        assert lib.rr_linear(C.byref(c), FAKE, FAKE, None, None, FAKE, None, FAKE, BIG, None) == want
+        assert lib.rr_linear_backward(C.byref(c), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, None, FAKE, BIG, None) == want
+
+
+def test_linear_refusals(lib):
+    c = _linear()
+    n = C.c_size_t(0)
+    assert lib.rr_linear_workspace_bytes(None, 0, C.byref(n)) == INVALID
+    assert lib.rr_linear_workspace_bytes(C.byref(c), 0, None) == INVALID
+    assert lib.rr_linear_workspace_bytes(C.byref(c), 2, C.byref(n)) == INVALID
+    good = dict(x=FAKE, w=FAKE, bias=FAKE, residual=FAKE, y=FAKE, pre=FAKE, ws=FAKE, size=BIG)
+
+    def forward(**kw):
+        a = dict(good, **kw)
+        return lib.rr_linear(C.byref(c), a["x"], a["w"], a["bias"], a["residual"], a["y"], a["pre"], a["ws"], a["size"], None)
+    for kw in (dict(x=None), dict(w=None), dict(y=None), dict(x=ODD16), dict(w=ODD16), dict(bias=ODD4), dict(residual=ODD16), dict(y=ODD16),
+               dict(pre=ODD16)):
+        assert forward(**kw) == INVALID, kw
+    for kw in (dict(ws=None), dict(ws=C.c_void_p(0x1010)), dict(size=0)):
+        assert forward(**kw) == WORKSPACE, kw
+    assert lib.rr_linear(None, FAKE, FAKE, None, None, FAKE, None, FAKE, BIG, None) == INVALID
+    good = dict(x=FAKE, w=FAKE, pre=FAKE, dy=FAKE, dx=FAKE, dw=FAKE, dbias=FAKE, ws=FAKE, size=BIG)
+
+    def backward(cfg=c, **kw):
+        a = dict(good, **kw)
+        return lib.rr_linear_backward(C.byref(cfg), a["x"], a["w"], a["pre"], a["dy"], a["dx"], a["dw"], a["dbias"], a["ws"], a["size"], None)
+    for kw in (dict(dy=None), dict(pre=None), dict(dx=None, dw=None, dbias=None), dict(x=None), dict(w=None), dict(x=ODD16), dict(w=ODD16),
+               dict(pre=ODD16), dict(dy=ODD16), dict(dx=ODD16), dict(dw=ODD16), dict(dbias=ODD4)):
+        assert backward(**kw) == INVALID, kw
+    for kw in (dict(ws=None), dict(ws=C.c_void_p(0x1010)), dict(size=0)):
+        assert backward(**kw) == WORKSPACE, kw
+
+
+def test_dropout_refusals(lib):
+    def call(n=64, dtype=rr.RR_BF16, x=FAKE, residual=None, p=0.1, dev=None, out=FAKE):
+        a = lib.rr_dropout(n, dtype, x, residual, p, 1, 2, dev, out, None)
+        if residual is None:
+            assert lib.rr_dropout_backward(n, dtype, x, p, 1, 2, dev, out, None) == a
+        return a
+    for kw in (dict(n=0), dict(n=-1), dict(x=None), dict(out=None), dict(p=-0.1), dict(p=1.5), dict(p=float("nan")), dict(x=ODD16), dict(out=ODD16),
+               dict(residual=ODD16), dict(dev=C.c_void_p(0x1004))):
+        assert call(**kw) == INVALID, kw
+    for kw in (dict(dtype=2), dict(n=(1 << 40) + 1)):
+        assert call(**kw) == UNSUPPORTED, kw
+
+
+def test_balance_refusals(lib):
+    cfg = lambda **kw: rr.RRConfig(**dict(dict(T=64, d_model=64, d_ff=0, E=8, k=2, G=2, capacity_factor=1.0), **kw)).c()
+    c, n = cfg(), C.c_size_t(0)
+    assert lib.rr_balance_workspace_bytes(C.byref(c), C.byref(n)) == 0 and n.value % 256 == 0
+    assert lib.rr_balance_workspace_bytes(C.byref(c), None) == INVALID and lib.rr_balance_workspace_bytes(None, C.byref(n)) == INVALID
+    good = dict(c=c, logits=FAKE, rank=FAKE, mask=None, coef=0.1, loss=FAKE, counts=FAKE, mean=FAKE, ws=FAKE, size=BIG)
+
+    def forward(**kw):
+        a = dict(good, **kw)
+        return lib.rr_balance_loss(C.byref(a["c"]), a["logits"], a["rank"], a["mask"], a["coef"], a["loss"], a["counts"], a["mean"], a["ws"],
+                                   a["size"], None)
+    for kw in (dict(logits=None), dict(rank=None), dict(loss=None), dict(counts=None), dict(coef=float("nan")), dict(coef=float("inf")),
+               dict(logits=ODD4), dict(rank=ODD4), dict(loss=ODD4), dict(counts=ODD4), dict(mean=ODD4), dict(c=cfg(T=0)), dict(c=cfg(k=9))):
+        assert forward(**kw) == INVALID, kw
+    for kw in (dict(ws=None), dict(ws=C.c_void_p(0x1010)), dict(size=0)):
+        assert forward(**kw) == WORKSPACE, kw
+    assert forward(c=cfg(E=128)) == UNSUPPORTED
+    other = C.c_void_p(0x2000)
+
+    def backward(c=c, logits=FAKE, counts=FAKE, coef=0.1, dloss=None, flags=0, dlogits=other):
+        return lib.rr_balance_loss_backward(C.byref(c), logits, counts, None, coef, dloss, flags, dlogits, None)
+    for kw in (dict(logits=None), dict(counts=None), dict(dlogits=None), dict(dlogits=FAKE), dict(coef=float("nan")), dict(flags=1), dict(flags=4),
+               dict(logits=ODD4), dict(counts=ODD4), dict(dloss=ODD4), dict(dlogits=ODD4), dict(c=cfg(T=0))):
+        assert backward(**kw) == INVALID, kw
+
+
+# ------------------------------------------------------------------ refusals of the binding
+
+def test_binding_refuses_tensors_off_the_gpu():
+    f = lambda *s: torch.zeros(s)
+    cfg = rr.RRLinearConfig(4, 8, 8, rr.RR_F32)
+    with pytest.raises(rr.RRError, match="not on the current GPU"):
+        rr.rr_linear(cfg, f(4, 8), f(8, 8), None, None, f(4, 8), None, torch.zeros(256, dtype=torch.uint8))
+    with pytest.raises(rr.RRError, match="not on the current GPU"):
+        rr.rr_linear_backward(cfg, f(4, 8), f(8, 8), None, f(4, 8), f(4, 8), None, None, torch.zeros(256, dtype=torch.uint8))
+    with pytest.raises(rr.RRError, match="not on the current GPU"):
+        rr.rr_dropout(f(8), 0.1, 1, 2, f(8))
+    with pytest.raises(rr.RRError, match="unsupported type"):
+        rr.rr_dropout_backward(f(8).half(), 0.1, 1, 2, f(8).half())
+    cfg = rr.RRConfig(4, 8, 0, 4, 2, 1, 1.0)
+    with pytest.raises(rr.RRError, match="not on the current GPU"):
+        rr.rr_balance_loss(cfg, f(4, 4), torch.zeros((4, 3), dtype=torch.int32), 0.1, f(1), torch.zeros(5, dtype=torch.int32),
+                           torch.zeros(256, dtype=torch.uint8))
+    with pytest.raises(rr.RRError, match="not on the current GPU"):
+        rr.rr_balance_loss_backward(cfg, f(4, 4), torch.zeros(5, dtype=torch.int32), 0.1, f(4, 4))
+    with pytest.raises(rr.RRError, match="unsupported dtype"):
+        rr.rr_linear(rr.RRLinearConfig(4, 8, 8, 7), f(4, 8), f(8, 8), None, None, f(4, 8), None, None)
+
+
+def test_struct_layout_matches_header():
+    assert C.sizeof(binding._LinearConfig) == 20
+    assert rr.RRLinearConfig(1, 8, 16, act=rr.RR_ACT_SWIGLU).rows == 32 and rr.RRLinearConfig(1, 8, 16).rows == 16
