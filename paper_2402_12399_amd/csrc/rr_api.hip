@@ -26,6 +26,7 @@ static int device_setup() {
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return -1;
   std::call_once(g_dev_once[dev], [dev] {
     hipError_t e = ffn_kernel_attributes();
+    if (e == hipSuccess) e = linear_kernel_attributes();
     if (e == hipSuccess) e = router_kernel_attributes();
     if (e == hipSuccess) e = dispatch_kernel_attributes();
     void *p = nullptr;

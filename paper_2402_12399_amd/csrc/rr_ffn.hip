@@ -210,9 +210,6 @@ FfnPlan ffn_plan(const Dims &D) {
   return best;
 }
 
-template <class S>
-struct Tag { using type = S; };
-
 template <class F>
 void for_each_tile_kernel(F f) {
   auto shape = [&](auto tag) {
@@ -227,16 +224,7 @@ void for_each_tile_kernel(F f) {
     f(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false>, S::SMEM);
     f(gemm_tile_kernel<S, false, -1, false, true>, S::SMEM);
   };
-  shape(Tag<TileS128>{});
-  shape(Tag<TileS64>{});
-  shape(Tag<TileF64>{});
-  shape(Tag<TileF32>{});
-  shape(Tag<TileF32n>{});
-  shape(Tag<TileB256>{});
-  shape(Tag<TileB128>{});
-  shape(Tag<TileB64>{});
-  shape(Tag<TileB32>{});
-  shape(Tag<TileB32n>{});
+  for_each_tile_shape(shape);
 }
 
 // bf16 SwiGLU layers whose activation is computed with a division, not the hardware's reciprocal

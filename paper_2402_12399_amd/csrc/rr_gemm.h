@@ -1129,6 +1129,23 @@ using TileB64 = TileShape<TILE_BF16, 2, 2, 2, 4, 3, 2>;      // bf16, 64 x 128
 using TileB32 = TileShape<TILE_BF16, 1, 2, 2, 4, 4, 2>;      // bf16, 32 x 128
 using TileB32n = TileShape<TILE_BF16, 1, 2, 2, 2, 5, 2>;     // bf16, 32 x 64
 
+template <class S>
+struct Tag { using type = S; };
+
+template <class F>
+void for_each_tile_shape(F shape) {
+  shape(Tag<TileS128>{});
+  shape(Tag<TileS64>{});
+  shape(Tag<TileF64>{});
+  shape(Tag<TileF32>{});
+  shape(Tag<TileF32n>{});
+  shape(Tag<TileB256>{});
+  shape(Tag<TileB128>{});
+  shape(Tag<TileB64>{});
+  shape(Tag<TileB32>{});
+  shape(Tag<TileB32n>{});
+}
+
 static_assert(TileB32::BM == kMinRowTile && TileB32n::BM == kMinRowTile && TileF32::BM == kMinRowTile && TileF32n::BM == kMinRowTile && LG_ROWS == kMinRowTile);
 
 // Which tiles a GEMM uses: the shape with the least estimated time.  A CU works through ceil(tiles / CUs) tiles of

@@ -171,6 +171,7 @@ hipError_t launch_balance_grad(int T, int E, int k, const float *logits, const i
 // m of 65536: random numbers below it drop their element
 hipError_t launch_dropout(long long n, int dtype, const void *x, const void *residual, u32 m, unsigned long long seed,
                           unsigned long long offset, const unsigned long long *device_offset, void *out, KernelId id, hipStream_t s);
+hipError_t linear_kernel_attributes();  // as ffn_kernel_attributes
 size_t linear_workspace(const rr_linear_config &c, bool backward);
 hipError_t launch_linear(const rr_linear_config &c, const void *x, const void *w, const float *bias, const void *residual, void *y,
                          void *pre, void *ws, hipStream_t s);

@@ -1,147 +1,457 @@
 // Dense projection: z = x W^T + bias, y = residual + act(z); gradients dx = dz W, dw = dz^T x, dbias = sum of dz's rows.
-// One kernel of 64 x 64 tiles, fp32 FMAs on operands of any strides, serves the three products.
-#include <algorithm>
-
-#include "rr_device.h"
+//
+// Every product is "A[rows, K] times B[N, K]^T" with K contiguous in both operands (rr_gemm.h):
+//   forward  x, W                 dx  dz, W^T                 dw  dz^T, x^T
+// The transposes are made by linear_turn_kernel, which also makes dz from dy and the stored z, and sums its columns.
+// Which kernel multiplies is a matter of estimated time (dense_plan): 256 x 256 tiles of the persistent kernel, smaller
+// tiles, either with the summation cut into slices where the tiles alone would leave CUs idle (each slice's raw sums go
+// to the workspace and linear_join_kernel adds them in order and does the epilogue), or, up to kFewRows rows,
+// linear_rows_kernel.
+#include "rr_gemm.h"
 
 namespace rr {
 
 namespace {
 
-constexpr int LN_TILE = 64, LN_K = 16, LN_THREADS = 256;
-
-// C[m, n] = sum_k A[m, k] B[n, k], operands with strides in elements.
-struct LinearArgs {
-  const void *A, *B;
-  long long am, ak, bn, bk;
-  int M, N, K;
-  const float *bias;     // epilogue
-  const void *residual;
-  void *out, *pre;
-  int act, Nout;         // RR_ACT_SWIGLU: column n < Nout of B is the gate's, n + Nout the up projection's
-};
+int width(const rr_linear_config &c) { return c.act == RR_ACT_SWIGLU ? 2 * c.N : c.N; }
+int element(const rr_linear_config &c) { return c.dtype == RR_BF16 ? 2 : 4; }
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 template <bool BF16>
-__device__ inline float load_value(const void *p, long long i) {
+__device__ inline float load_value(const void *p, size_t i) {
   if (BF16) return __builtin_bit_cast(float, (u32) static_cast<const uint16_t *>(p)[i] << 16);
   return static_cast<const float *>(p)[i];
 }
-template <bool BF16>
-__device__ inline void store_value(void *p, long long i, float v) {
-  if (BF16) static_cast<uint16_t *>(p)[i] = (uint16_t)pack_bf16(v, 0.0f);
-  else static_cast<float *>(p)[i] = v;
-}
 
-template <bool BF16, bool GATED>
-__global__ __launch_bounds__(LN_THREADS) void linear_tile_kernel(LinearArgs P) {
-  constexpr int NB = GATED ? 2 : 1;
-  __shared__ float a[LN_K][LN_TILE + 1], b[NB][LN_K][LN_TILE + 1];
-  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-  const int m0 = blockIdx.y * LN_TILE, n0 = blockIdx.x * LN_TILE;
-  float acc[NB][4][4] = {};
-  for (int k0 = 0; k0 < P.K; k0 += LN_K) {
-    for (int i = tid; i < LN_K * LN_TILE; i += LN_THREADS) {
-      const int r = i / LN_K, k = i % LN_K;
-      const bool kin = k0 + k < P.K;
-      a[k][r] = kin && m0 + r < P.M ? load_value<BF16>(P.A, (m0 + r) * P.am + (k0 + k) * P.ak) : 0.0f;
+// ------------------------------------------------------------------ few rows
+// One to kFewRows rows: the weights are read once and everything else is small.  A workgroup owns 16 columns (gated: of both
+// halves of W), its waves take turns at chunks of 64 (fp32: 32) elements of the rows and load fragments straight from
+// global memory, without LDS, chunks ahead; the waves' sums are added through LDS in order.
+constexpr int kFewRows = 32;
+constexpr int LR_NW = 8, LR_THREADS = LR_NW * 64, LR_AHEAD = 4;
+
+template <bool BF16, bool GATED, int ACT, int MF>
+__global__ __launch_bounds__(LR_THREADS, 2) void linear_rows_kernel(DenseArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int ES = BF16 ? 2 : 4, NB = GATED ? 2 : 1, CHUNK = 128;  // bytes of a row
+  using Frag = typename std::conditional<BF16, bf16x8, f32x4>::type;
+  __shared__ f32x4 red[LR_NW][MF * NB][64];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, q = lane >> 4;
+  const int N = P.N, n0 = blockIdx.x * 16;
+  const unsigned rowb = (unsigned)P.K * ES;
+  const int chunks = (int)((rowb + CHUNK - 1) / CHUNK);
+  auto rsrc = [](const void *base, size_t off, size_t range) {
+    return __builtin_amdgcn_make_buffer_rsrc(static_cast<char *>(const_cast<void *>(base)) + off, 0,
+                                             __builtin_amdgcn_readfirstlane((int)range), BUF_FLAGS);
+  };
+  // rows past the last one and pieces past a row's end read as zero
+  const __amdgpu_buffer_rsrc_t rsA = rsrc(P.A, 0, (size_t)P.M * rowb);
+  const size_t wrows = (size_t)min(16, N - n0) * rowb;
+  const __amdgpu_buffer_rsrc_t rsB[2] = {rsrc(P.B0, (size_t)n0 * rowb, wrows), GATED ? rsrc(P.B1, (size_t)n0 * rowb, wrows) : rsA};
+  constexpr unsigned PAST = 0x7ffffff0u;
+  auto load = [](const __amdgpu_buffer_rsrc_t &rs, unsigned off) {
+    return __builtin_bit_cast(Frag, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
+  };
+  f32x4 acc[MF][NB];
 #pragma unroll
-      for (int q = 0; q < NB; ++q)
-        b[q][k][r] = kin && n0 + r < P.N ? load_value<BF16>(P.B, (long long)(n0 + r + q * P.Nout) * P.bn + (k0 + k) * P.bk) : 0.0f;
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  Frag a[LR_AHEAD][2][MF], b[LR_AHEAD][2][NB];
+  auto fetch = [&](int c, int slot) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const unsigned at = (unsigned)c * CHUNK + h * 64 + q * 16;
+      const bool in = c < chunks && at < rowb;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) b[slot][h][j] = load(rsB[j], in ? r * rowb + at : PAST);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) a[slot][h][i] = load(rsA, in && i * 16 + r < P.M ? (i * 16 + r) * rowb + at : PAST);
     }
-    __syncthreads();
+  };
 #pragma unroll
-    for (int k = 0; k < LN_K; ++k)
+  for (int s = 0; s < LR_AHEAD; ++s) fetch(w + s * LR_NW, s);
+  for (int c = w; c < chunks; c += LR_AHEAD * LR_NW) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int s = 0; s < LR_AHEAD; ++s) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int q = 0; q < NB; ++q) acc[q][i][j] = fmaf(a[k][ty + 16 * i], b[q][k][tx + 16 * j], acc[q][i][j]);
-    __syncthreads();
+        for (int i = 0; i < MF; ++i)
+#pragma unroll
+          for (int j = 0; j < NB; ++j) {
+            // B fragment first, as in the other kernels: lane owns row (lane & 15), columns 4 * (lane >> 4) .. + 3
+            if constexpr (BF16) {
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[s][h][j], a[s][h][i], acc[i][j], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[s][h][j][u], a[s][h][i][u], acc[i][j], 0, 0, 0);
+            }
+          }
+      fetch(c + (LR_AHEAD + s) * LR_NW, s);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < MF; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-      if (m >= P.M || n >= P.N) continue;
-      float z[NB];
-#pragma unroll
-      for (int q = 0; q < NB; ++q) {
-        z[q] = acc[q][i][j] + (P.bias ? P.bias[n + q * P.Nout] : 0.0f);
-        if (P.pre) store_value<BF16>(P.pre, (long long)m * NB * P.Nout + n + q * P.Nout, z[q]);
-      }
-      float y = z[0];
-      if (GATED) y = z[0] / (1.0f + expf(-z[0])) * z[NB - 1];
-      else if (P.act == RR_ACT_GELU) y = gelu_erf(z[0]);
-      const long long at = (long long)m * P.N + n;
-      if (P.residual) y += load_value<BF16>(P.residual, at);
-      store_value<BF16>(P.out, at, y);
-    }
-}
-
-// dz = dy act'(z) and, per 64 columns, the column sums.
-template <bool BF16>
-__global__ __launch_bounds__(256) void linear_dz_kernel(const void *dy, const void *pre, int act, int M, int N, void *dz, float *dbias) {
-  __shared__ double sums[2][4][kWave];
-  const int lane = threadIdx.x & 63, part = threadIdx.x >> 6, n = blockIdx.x * kWave + lane;
-  const bool gated = act == RR_ACT_SWIGLU;
-  const int R = gated ? 2 * N : N;
-  double s0 = 0.0, s1 = 0.0;
-  if (n < N)
-    for (int m = part; m < M; m += 4) {
-      const float d = load_value<BF16>(dy, (long long)m * N + n);
-      float g = d, u = 0.0f;
-      if (act != RR_ACT_NONE) {
-        const float z = load_value<BF16>(pre, (long long)m * R + n);
-        if (gated) {
-          const float up = load_value<BF16>(pre, (long long)m * R + N + n), t = 1.0f / (1.0f + expf(-z));
-          g = d * up * t * (1.0f + z * (1.0f - t));
-          u = d * z * t;
-          if (dz) store_value<BF16>(dz, (long long)m * R + N + n, u);
-        } else {
-          g = d * (0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z));
-        }
-        if (dz) store_value<BF16>(dz, (long long)m * R + n, g);
-      }
-      s0 += g;
-      s1 += u;
-    }
-  sums[0][part][lane] = s0;
-  sums[1][part][lane] = s1;
+    for (int j = 0; j < NB; ++j) red[w][i * NB + j][lane] = acc[i][j];
   __syncthreads();
-  if (part > 0 || n >= N || !dbias) return;
-  s0 = s1 = 0.0;
-  for (int q = 0; q < 4; ++q) {
-    s0 += sums[0][q][lane];
-    s1 += sums[1][q][lane];
+  if (w >= MF) return;
+  f32x4 sum[1][NB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    sum[0][j] = red[0][w * NB + j][lane];
+#pragma unroll
+    for (int s = 1; s < LR_NW; ++s) sum[0][j] += red[s][w * NB + j][lane];
   }
-  dbias[n] = (float)s0;
-  if (gated) dbias[N + n] = (float)s1;
+  store_dense<1, NB, 16, BF16, GATED, ACT>(sum, P, 0, w * 16 + r, P.M, n0, lane);
+#endif
 }
 
-void launch_tile(bool bf16, bool gated, const LinearArgs &A, hipStream_t s) {
-  const dim3 grid((A.N + LN_TILE - 1) / LN_TILE, (A.M + LN_TILE - 1) / LN_TILE);
-  if (bf16 && gated) linear_tile_kernel<true, true><<<grid, LN_THREADS, 0, s>>>(A);
-  else if (bf16) linear_tile_kernel<true, false><<<grid, LN_THREADS, 0, s>>>(A);
-  else if (gated) linear_tile_kernel<false, true><<<grid, LN_THREADS, 0, s>>>(A);
-  else linear_tile_kernel<false, false><<<grid, LN_THREADS, 0, s>>>(A);
+// ------------------------------------------------------------------ joining slices
+// Adds the slices' sums in order and does the epilogue; a thread owns four columns (gated: of both halves).
+template <bool BF16, bool GATED, int ACT>
+__global__ __launch_bounds__(256) void linear_join_kernel(DenseArgs P) {
+  const int N = P.N, R = GATED ? 2 * N : N, quads = N / 4;
+  const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= (size_t)P.M * quads) return;
+  const int row = (int)(t / quads), col = (int)(t - (size_t)row * quads) * 4;
+  f32x4 acc[1][GATED ? 2 : 1];
+#pragma unroll
+  for (int j = 0; j < (GATED ? 2 : 1); ++j) {
+    const float *at = P.part + (size_t)row * R + j * N + col;
+    acc[0][j] = *reinterpret_cast<const f32x4 *>(at);
+    for (int s = 1; s < P.slices; ++s) acc[0][j] += *reinterpret_cast<const f32x4 *>(at + (size_t)s * P.M * R);
+  }
+  DenseArgs Q = P;
+  Q.part = nullptr;
+  // lane 0 .. 15 of a fragment own its first four columns: the thread's four, as if it were such a lane
+  store_dense<1, GATED ? 2 : 1, 16, BF16, GATED, ACT>(acc, Q, 0, row, P.M, col, 0);
 }
 
-int width(const rr_linear_config &c) { return c.act == RR_ACT_SWIGLU ? 2 * c.N : c.N; }
+// ------------------------------------------------------------------ dz, transposes, column sums
+// A workgroup takes 64 rows x 64 columns of dy (or of x, or W: ACT none), makes dz where there is an activation, and
+// writes what is asked for: dz, its transpose of row pitch LT >= M (zeros behind column M), the sums of its columns over
+// the 64 rows.  A thread owns two neighbouring rows and eight columns, so that the transpose goes through LDS in words.
+// Bound by HBM.
+struct TurnArgs {
+  const void *src, *pre;  // [M, N], [M, R]
+  void *dz, *turned;      // [M, R], [R, LT]
+  float *sums;            // [row blocks, R]
+  int M, N, LT;
+};
+constexpr int TN_TILE = 64, TN_THREADS = 256;
+
+template <bool BF16>
+__device__ inline void load_eight(const void *p, size_t at, bool in, float (&v)[8]) {
+  if constexpr (BF16) {
+    const uint4 q = in ? *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(p) + at) : make_uint4(0, 0, 0, 0);
+    const u32 w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float, i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  } else {
+    const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float4 *s = reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at);
+    const float4 a = in ? s[0] : z, b = in ? s[1] : z;
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+template <bool BF16>
+__device__ inline void store_eight(void *p, size_t at, const float (&v)[8]) {
+  if constexpr (BF16) {
+    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(p) + at) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  } else {
+    float4 *d = reinterpret_cast<float4 *>(static_cast<float *>(p) + at);
+    d[0] = make_float4(v[0], v[1], v[2], v[3]);
+    d[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+}
+
+template <bool BF16, int ACT>
+__global__ __launch_bounds__(TN_THREADS) void linear_turn_kernel(TurnArgs P) {
+  constexpr int NB = ACT == RR_ACT_SWIGLU ? 2 : 1;
+  constexpr int PITCH = BF16 ? TN_TILE / 2 + 1 : TN_TILE + 1;  // words of a column in LDS: odd, so that no two lanes meet in a bank
+  __shared__ u32 tile[TN_TILE * PITCH];
+  __shared__ float part[TN_THREADS / kWave][TN_TILE];
+  const int tid = threadIdx.x, piece = tid & 7, pair = tid >> 3, N = P.N, R = NB * N;
+  const int n0 = blockIdx.x * TN_TILE, m0 = blockIdx.y * TN_TILE, col = n0 + piece * 8, row = m0 + 2 * pair;
+  float v[NB][2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const bool in = row + h < P.M && col < N;
+    load_eight<BF16>(P.src, (size_t)(row + h) * N + col, in, v[0][h]);
+    if constexpr (ACT != RR_ACT_NONE) {
+      float z[8], up[8];
+      load_eight<BF16>(P.pre, (size_t)(row + h) * R + col, in, z);
+      if constexpr (NB == 2) load_eight<BF16>(P.pre, (size_t)(row + h) * R + N + col, in, up);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float d = v[0][h][i];
+        if constexpr (NB == 2) {
+          // silu' = t (1 + z (1 - t)), t = 1 / (1 + exp(-z))
+          const float t = 1.0f / (1.0f + (BF16 ? __expf(-z[i]) : expf(-z[i])));
+          v[0][h][i] = d * up[i] * t * (1.0f + z[i] * (1.0f - t));
+          v[NB - 1][h][i] = d * z[i] * t;
+        } else {
+          v[0][h][i] = d * (0.5f * (1.0f + erff(z[i] * 0.70710678118654752f)) + z[i] * 0.39894228040143268f * expf(-0.5f * z[i] * z[i]));
+        }
+      }
+      if (P.dz && in)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) store_eight<BF16>(P.dz, (size_t)(row + h) * R + b * N + col, v[b][h]);
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    if (P.sums) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float s = v[b][0][i] + v[b][1][i];
+#pragma unroll
+        for (int o = 8; o < kWave; o <<= 1) s += __shfl_xor(s, o);
+        if ((tid & (kWave - 1)) < 8) part[tid >> 6][piece * 8 + i] = s;
+      }
+      __syncthreads();
+      if (tid < TN_TILE && n0 + tid < N)
+        P.sums[(size_t)blockIdx.y * R + b * N + n0 + tid] = (part[0][tid] + part[1][tid]) + (part[2][tid] + part[3][tid]);
+    }
+    if (P.turned) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        u32 *at = tile + (piece * 8 + i) * PITCH;
+        if constexpr (BF16) {
+          at[pair] = pack_bf16(v[b][0][i], v[b][1][i]);
+        } else {
+          at[2 * pair] = __builtin_bit_cast(u32, v[b][0][i]);
+          at[2 * pair + 1] = __builtin_bit_cast(u32, v[b][1][i]);
+        }
+      }
+      __syncthreads();
+      constexpr int WORDS = BF16 ? TN_TILE / 2 : TN_TILE, PIECES = WORDS / 4;  // of a turned row; 16-byte pieces
+#pragma unroll
+      for (int k = 0; k < TN_TILE * PIECES / TN_THREADS; ++k) {
+        const int p = k * TN_THREADS + tid, c = p / PIECES, q = p % PIECES;
+        const u32 *at = tile + c * PITCH + q * 4;
+        const int m = m0 + q * (BF16 ? 8 : 4);
+        if (n0 + c < N && m < P.LT)
+          *reinterpret_cast<uint4 *>(static_cast<char *>(P.turned) + ((size_t)(b * N + n0 + c) * P.LT + m) * (BF16 ? 2 : 4)) =
+              make_uint4(at[0], at[1], at[2], at[3]);
+      }
+    }
+    if (b + 1 < NB) __syncthreads();
+  }
+}
+
+// dbias from the row blocks' sums, in order.
+__global__ __launch_bounds__(256) void linear_bias_kernel(const float *sums, int blocks, int R, float *dbias) {
+  __shared__ double part[4][kWave];
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6, n = blockIdx.x * kWave + lane;
+  double s = 0.0;
+  if (n < R)
+    for (int i = q; i < blocks; i += 4) s += (double)sums[(size_t)i * R + n];
+  part[q][lane] = s;
+  __syncthreads();
+  if (q == 0 && n < R) dbias[n] = (float)((part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+}
+
+// ------------------------------------------------------------------ which kernel
+constexpr int kMaxSlices = 16;
+constexpr size_t kPartBytes = (size_t)128 << 20;  // most that slices' sums may take
+size_t part_bytes(size_t M, size_t R, int slices) { return M * R * 4 * slices; }
+// the workspace for them: of a product of M rows it also serves every product of fewer rows
+size_t part_reserve(size_t M, size_t R) { return up256(std::min(part_bytes(M, R, kMaxSlices), kPartBytes)); }
+
+struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_kernel
+
+// Estimated time (us) of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
+// The numbers are the grouped GEMM's (kShape); the row tiles are known here.
+float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, int q, int slices) {
+  constexpr int kCUs = 256;
+  const ShapeInfo &s = kShape[q];
+  const int es = bf16 ? 2 : 4, ce = GB_ROW_BYTES / es, bn = gated ? s.brows / 2 : s.brows;
+  const long long Ks = slices > 1 ? (K / slices + ce - 1) / ce * ce : K;
+  if (slices > 1 && (Ks * slices < K || Ks * (slices - 1) >= K)) return -1.0f;
+  const bool persistent = q == FFN_P256, split = q == FFN_S128 || q == FFN_S64;
+  if (persistent && (!persistent_ok((int)Ks) || (slices > 1 && Ks * slices != K))) return -1.0f;
+  const int KT = (int)((Ks + ce - 1) / ce);
+  if (split && KT < 5) return -1.0f;
+  const long long mt = (M + s.bm - 1) / s.bm, nt = (N + bn - 1) / bn, tiles = mt * nt * slices, rounds = tiles / kCUs, left = tiles - rounds * kCUs;
+  const size_t R = (size_t)N * (gated ? 2 : 1);
+  if (slices > 1 && part_bytes(M, R, slices) > kPartBytes) return -1.0f;
+  const float stream = (float)((double)(M + R) * K * es + (double)M * N * es) / kHbm;
+  const float fetch = (float)GB_ROW_BYTES * ((float)s.brows / mt + (float)s.bm / nt) / kCuFetch;
+  const float chunk = std::max(s.cost, fetch), fixed = s.fixed;
+  float busy = (float)rounds * (KT * chunk + fixed);
+  if (split) {
+    const float all = (float)tiles / kCUs;
+    busy = std::max((0.56f * all + 0.44f * ceilf(all)) * (KT * chunk + fixed), KT * s.alone + fixed);
+  } else if (persistent) {
+    busy += kPersistentStart;
+    if (left > 0) busy += KT * std::max(s.cost * kCutCost[std::min<long long>(kCUs / left, PK_MAX_CUT) - 1], fetch) + fixed;
+  } else if (left > 0) {
+    busy += (KT * chunk + fixed) * (rounds ? std::min(1.0f, (float)left / kCUs + 0.5f) : 1.0f);
+  }
+  float t = std::max(busy, stream) + 0.1f * busy;
+  if (slices > 1) t += 4.0f + (float)part_bytes(M, R, slices) * 2.0f / kHbm;
+  return t;
+}
+
+DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated) {
+  if (M <= kFewRows) return {-1, 1};
+  const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : FFN_F32N;
+  DensePlan best{q1, 1};
+  float least = -1.0f;
+  for (int q = q0; q <= q1; ++q)
+    for (int s = 1; s <= kMaxSlices; ++s) {
+      const float t = dense_cost(M, N, K, bf16, gated, q, s);
+      if (t >= 0.0f && (least < 0.0f || t < least)) { least = t; best = {q, s}; }
+    }
+  return best;
+}
+
+template <class S, bool GATED, int ACT>
+void launch_dense_tiles(DenseArgs A, hipStream_t s) {
+  constexpr int bn = GATED ? S::BROWS / 2 : S::BROWS;
+  A.NT = (A.N + bn - 1) / bn;
+  A.MT = (A.M + S::BM - 1) / S::BM;
+  constexpr long long kRow = 1ll << 20;  // workgroups in a row of the grid, whole XCD runs (see gemm_tile_kernel)
+  const long long tiles = (long long)A.NT * A.MT * A.slices;
+  const dim3 grid((unsigned)((std::min(tiles, kRow) + 7) / 8 * 8), (unsigned)((tiles + kRow - 1) / kRow));
+  gemm_tile_kernel<S, GATED, ACT, false, false, true><<<grid, S::THREADS, S::SMEM, s>>>(A);
+}
+
+template <bool BF16, bool GATED, int ACT>
+void launch_dense_shape(int shape, const DenseArgs &A0, hipStream_t s) {
+  DenseArgs A = A0;
+  if constexpr (BF16) {
+    switch (shape) {
+      case FFN_P256:
+        A.NT = GATED ? (A.N + 127) / 128 : (A.N + 255) / 256;
+        A.MT = (A.M + PK_BM - 1) / PK_BM;
+        gemm_bf16_persistent_kernel<GATED, ACT, false, false, true><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
+        break;
+      case FFN_256: launch_dense_tiles<TileB256, GATED, ACT>(A, s); break;
+      case FFN_128: launch_dense_tiles<TileB128, GATED, ACT>(A, s); break;
+      case FFN_64: launch_dense_tiles<TileB64, GATED, ACT>(A, s); break;
+      case FFN_32: launch_dense_tiles<TileB32, GATED, ACT>(A, s); break;
+      default: launch_dense_tiles<TileB32n, GATED, ACT>(A, s); break;
+    }
+  } else {
+    switch (shape) {
+      case FFN_S128: launch_dense_tiles<TileS128, GATED, ACT>(A, s); break;
+      case FFN_S64: launch_dense_tiles<TileS64, GATED, ACT>(A, s); break;
+      case FFN_F64: launch_dense_tiles<TileF64, GATED, ACT>(A, s); break;
+      case FFN_F32: launch_dense_tiles<TileF32, GATED, ACT>(A, s); break;
+      default: launch_dense_tiles<TileF32n, GATED, ACT>(A, s); break;
+    }
+  }
+}
+
+// The product and its epilogue.  A.A, B0, B1, Cout, M, N, LD, Kall and the epilogue's pointers are set.
+template <bool BF16, bool GATED, int ACT>
+void launch_product(DenseArgs A, float *part, hipStream_t s) {
+  const DensePlan plan = dense_plan(A.M, A.N, A.Kall, BF16, GATED);
+  constexpr int ce = GB_ROW_BYTES / (BF16 ? 2 : 4);
+  A.slices = plan.slices;
+  A.K = plan.slices > 1 ? (A.Kall / plan.slices + ce - 1) / ce * ce : A.Kall;
+  A.part = plan.slices > 1 ? part : nullptr;
+  if (plan.shape < 0) {
+    const dim3 grid((A.N + 15) / 16);
+    if (A.M <= 16) linear_rows_kernel<BF16, GATED, ACT, 1><<<grid, LR_THREADS, 0, s>>>(A);
+    else linear_rows_kernel<BF16, GATED, ACT, 2><<<grid, LR_THREADS, 0, s>>>(A);
+    return;
+  }
+  launch_dense_shape<BF16, GATED, ACT>(plan.shape, A, s);
+  if (plan.slices > 1)
+    linear_join_kernel<BF16, GATED, ACT><<<(unsigned)(((size_t)A.M * (A.N / 4) + 255) / 256), 256, 0, s>>>(A);
+}
+
+template <bool BF16>
+void launch_forward(int act, const DenseArgs &A, float *part, hipStream_t s) {
+  if (act == RR_ACT_SWIGLU) launch_product<BF16, true, -1>(A, part, s);
+  else if (act == RR_ACT_GELU) launch_product<BF16, false, RR_ACT_GELU>(A, part, s);
+  else launch_product<BF16, false, -1>(A, part, s);
+}
+
+template <bool BF16>
+void launch_turn(int act, const TurnArgs &A, hipStream_t s) {
+  const int rows = A.turned ? std::max(A.M, A.LT) : A.M;
+  const dim3 grid((A.N + TN_TILE - 1) / TN_TILE, (rows + TN_TILE - 1) / TN_TILE);
+  if (act == RR_ACT_SWIGLU) linear_turn_kernel<BF16, RR_ACT_SWIGLU><<<grid, TN_THREADS, 0, s>>>(A);
+  else if (act == RR_ACT_GELU) linear_turn_kernel<BF16, RR_ACT_GELU><<<grid, TN_THREADS, 0, s>>>(A);
+  else linear_turn_kernel<BF16, RR_ACT_NONE><<<grid, TN_THREADS, 0, s>>>(A);
+}
+
+// Workspace of the backward pass.
+struct BackwardWork {
+  void *dz, *dz_turned, *x_turned, *w_turned;
+  float *sums, *part;
+  int LT;  // row pitch of the transposes that are summed over rows: M and zeros up to whole chunks
+  size_t bytes;
+};
+BackwardWork backward_work(const rr_linear_config &c, void *ws) {
+  BackwardWork W;
+  char *base = static_cast<char *>(ws);
+  size_t off = 0;
+  auto take = [&](size_t n) {
+    void *p = base ? base + off : nullptr;
+    off += up256(n);
+    return p;
+  };
+  const size_t R = width(c), es = element(c);
+  W.LT = (c.M + 63) / 64 * 64;
+  W.dz = take(c.act == RR_ACT_NONE ? 0 : (size_t)c.M * R * es);
+  W.dz_turned = take(R * W.LT * es);
+  W.x_turned = take((size_t)c.K * W.LT * es);
+  W.w_turned = take((size_t)c.K * R * es);
+  W.sums = static_cast<float *>(take((size_t)(W.LT / TN_TILE) * R * 4));
+  W.part = static_cast<float *>(take(std::max(part_reserve(c.M, c.K), part_reserve(R, c.K))));
+  W.bytes = off;
+  return W;
+}
 
 }  // namespace
 
+hipError_t linear_kernel_attributes() {
+  hipError_t e = hipSuccess;
+  auto set = [&e](auto kern, int bytes) {
+    if (e == hipSuccess) e = set_lds(kern, bytes);
+  };
+  auto kinds = [&](auto tag) {
+    using S = typename decltype(tag)::type;
+    set(gemm_tile_kernel<S, true, -1, false, false, true>, S::SMEM);
+    set(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false, true>, S::SMEM);
+    set(gemm_tile_kernel<S, false, -1, false, false, true>, S::SMEM);
+  };
+  for_each_tile_shape(kinds);
+  set(gemm_bf16_persistent_kernel<true, -1, false, false, true>, PK_SMEM);
+  set(gemm_bf16_persistent_kernel<false, RR_ACT_GELU, false, false, true>, PK_SMEM);
+  set(gemm_bf16_persistent_kernel<false, -1, false, false, true>, PK_SMEM);
+  return e;
+}
+
 size_t linear_workspace(const rr_linear_config &c, bool backward) {
-  if (!backward || c.act == RR_ACT_NONE) return 256;
-  return ((size_t)c.M * width(c) * (c.dtype == RR_BF16 ? 2 : 4) + 255) / 256 * 256;
+  return backward ? backward_work(c, nullptr).bytes : std::max<size_t>(256, part_reserve(c.M, width(c)));
 }
 
 hipError_t launch_linear(const rr_linear_config &c, const void *x, const void *w, const float *bias, const void *residual, void *y,
-                         void *pre, void *, hipStream_t s) {
-  const LinearArgs A{x, w, c.K, 1, c.K, 1, c.M, c.N, c.K, bias, residual, y, pre, c.act, c.N};
+                         void *pre, void *ws, hipStream_t s) {
+  DenseArgs A{};
+  A.A = x;
+  A.B0 = w;
+  A.B1 = static_cast<const char *>(w) + (size_t)c.N * c.K * element(c);
+  A.Cout = y;
+  A.M = c.M;
+  A.N = c.N;
+  A.LD = A.Kall = c.K;
+  A.bias = bias;
+  A.residual = residual;
+  A.pre = pre;
   prof_begin(K_LINEAR, s);
-  launch_tile(c.dtype == RR_BF16, c.act == RR_ACT_SWIGLU, A, s);
+  if (c.dtype == RR_BF16) launch_forward<true>(c.act, A, static_cast<float *>(ws), s);
+  else launch_forward<false>(c.act, A, static_cast<float *>(ws), s);
   prof_end(K_LINEAR, s);
   return hipGetLastError();
 }
@@ -150,16 +460,34 @@ hipError_t launch_linear_backward(const rr_linear_config &c, const void *x, cons
                                   void *dw, float *dbias, void *ws, hipStream_t s) {
   const bool bf16 = c.dtype == RR_BF16;
   const int R = width(c);
-  const bool products = dx || dw;
-  const void *dz = c.act == RR_ACT_NONE ? dy : ws;
+  const BackwardWork W = backward_work(c, ws);
+  auto turn = [&](int act, const TurnArgs &A) {
+    if (bf16) launch_turn<true>(act, A, s);
+    else launch_turn<false>(act, A, s);
+  };
+  auto product = [&](const void *a, const void *b, void *out, int M, int N, int K) {
+    DenseArgs A{};
+    A.A = a;
+    A.B0 = A.B1 = b;
+    A.Cout = out;
+    A.M = M;
+    A.N = N;
+    A.LD = A.Kall = K;
+    if (bf16) launch_product<true, false, -1>(A, W.part, s);
+    else launch_product<false, false, -1>(A, W.part, s);
+  };
+  const bool act = c.act != RR_ACT_NONE;
   prof_begin(K_LINEAR_BWD, s);
-  if (dbias || (products && c.act != RR_ACT_NONE)) {
-    const dim3 grid((c.N + kWave - 1) / kWave);
-    if (bf16) linear_dz_kernel<true><<<grid, 256, 0, s>>>(dy, pre, c.act, c.M, c.N, products ? ws : nullptr, dbias);
-    else linear_dz_kernel<false><<<grid, 256, 0, s>>>(dy, pre, c.act, c.M, c.N, products ? ws : nullptr, dbias);
+  if (dw || dbias || (dx && act)) turn(c.act, TurnArgs{dy, pre, dx ? W.dz : nullptr, dw ? W.dz_turned : nullptr, dbias ? W.sums : nullptr, c.M, c.N, W.LT});
+  if (dbias) linear_bias_kernel<<<(R + kWave - 1) / kWave, 256, 0, s>>>(W.sums, (c.M + TN_TILE - 1) / TN_TILE, R, dbias);
+  if (dx) {
+    turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
+    product(act ? W.dz : dy, W.w_turned, dx, c.M, c.K, R);
   }
-  if (dx) launch_tile(bf16, false, LinearArgs{dz, w, R, 1, 1, c.K, c.M, c.K, R, nullptr, nullptr, dx, nullptr, RR_ACT_NONE, c.K}, s);
-  if (dw) launch_tile(bf16, false, LinearArgs{dz, x, 1, R, 1, c.K, R, c.K, c.M, nullptr, nullptr, dw, nullptr, RR_ACT_NONE, c.K}, s);
+  if (dw) {
+    turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
+    product(W.dz_turned, W.x_turned, dw, R, c.K, W.LT);
+  }
   prof_end(K_LINEAR_BWD, s);
   return hipGetLastError();
 }

@@ -405,7 +405,11 @@ def test_linear_infinities_and_nan_stay_in_their_rows(M, K, N, dtype):
     rows[2] = rows[4] = False
     cols = torch.ones(N, dtype=torch.bool, device="cuda")
     cols[9] = False
-    assert torch.equal(y[rows][:, cols], clean[rows][:, cols])
+    # fp32 rows next to a number that is not finite may be summed another way: both results are within the bound of the exact one
+    x[2], x[4], w[9] = 0.0, 0.0, 0.0
+    a = torch.mm(x.double().abs(), w.double().abs().t()) + b.double().abs()
+    both = 2 * linear_bound(a, K + 1, clean.double(), dtype) if dtype == "f32" else torch.zeros_like(a)
+    within(y[rows][:, cols], clean[rows][:, cols].double(), both[rows][:, cols], "rows and columns without them")
     assert bool(y[2].isnan().all()) and not bool(torch.isfinite(y[4]).any()) and not bool(torch.isfinite(y[:, 9]).any())
 
 
