@@ -254,29 +254,59 @@ def rr_router_backward(cfg: RRConfig, dout, logits, tables: Tables | None, works
                                              _ptr(dcombine_w), _ptr(dlogits), _stream()), "rr_router_backward")
 
 
-def _size(t) -> int:
-    return 0 if t is None else t.numel()
+class _Args:
+    """Addresses of the tensors of one call of the operators around the layer, checked: dense, as large as the call takes them to
+    be, of their type, and on the current device, where the call is enqueued.  (A few tenths of a microsecond per tensor: small
+    calls are bound by what the host does.)"""
 
+    __slots__ = ("what", "device")
 
-def _tensors(what: str, **checked):
-    """The operators around the layer: every tensor (or None) is dense, as large as the call takes it to be, of its type, and on
-    the current device, where the call is enqueued.  checked: name -> (tensor, elements, torch types)."""
-    import torch
-    for name, (t, numel, dtypes) in checked.items():
+    def __init__(self, what: str):
+        import torch
+        self.what = what
+        self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+
+    def __call__(self, name, t, numel, dtype):
+        """Address of t, or None for None."""
         if t is None:
-            continue
-        if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
-            raise RRError(f"{what}: {name} is on {t.device}, not on the current GPU")
-        if t.dtype not in dtypes or t.numel() != numel or not t.is_contiguous():
-            raise RRError(f"{what}: {name} must be dense, {numel} elements of {' or '.join(map(str, dtypes))}; "
-                          f"got {tuple(t.shape)} {t.dtype}")
+            return None
+        if not t.is_cuda or t.get_device() != self.device:
+            self._refuse_device(name, t)
+        if t.numel() != numel or t.dtype is not dtype or not t.is_contiguous():
+            raise RRError(f"{self.what}: {name} must be dense, {numel} elements of {dtype}; got {tuple(t.shape)} {t.dtype}, "
+                          f"{'dense' if t.is_contiguous() else 'not dense'}")
+        return t.data_ptr()
+
+    def workspace(self, t):
+        """Address and bytes of a workspace (None, 0 for None)."""
+        if t is None:
+            return None, 0
+        import torch
+        n = t.numel()
+        return self("workspace", t, n, torch.uint8), n
+
+    def mask(self, t, numel):
+        import torch
+        return self("token_mask", t, numel, torch.bool if t is not None and t.dtype is torch.bool else torch.uint8)
+
+    def stream(self):
+        import torch
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def _refuse_device(self, name, t):
+        import torch
+        # (a tensor on a GPU, though the module says that it has not been initialised: initialise it and look again)
+        if t.is_cuda and self.device is None:
+            self.device = torch.cuda.current_device()
+        if not t.is_cuda or t.get_device() != self.device:
+            raise RRError(f"{self.what}: {name} is on {t.device}, not on the current GPU")
 
 
 def _torch_type(dtype: int):
     import torch
     if dtype not in (RR_F32, RR_BF16):
         raise RRError(f"unsupported dtype {dtype}")
-    return (torch.float32 if dtype == RR_F32 else torch.bfloat16,)
+    return torch.float32 if dtype == RR_F32 else torch.bfloat16
 
 
 def rr_balance_workspace_bytes(cfg: RRConfig) -> int:
@@ -294,54 +324,47 @@ def rr_balance_loss(cfg: RRConfig, logits, rank_expert, coef: float, loss, count
     """loss [1], counts [E + 1] (int32: choices per expert, then the tokens that count), mean_prob [E] or None.
     token_mask [T], uint8 or bool, or None: 0 = padding."""
     import torch
-    f32, i32 = (torch.float32,), (torch.int32,)
-    _tensors("rr_balance_loss", logits=(logits, cfg.T * cfg.E, f32), rank_expert=(rank_expert, cfg.T * (cfg.k + 1), i32),
-             token_mask=(token_mask, cfg.T, (torch.uint8, torch.bool)), loss=(loss, 1, f32), counts=(counts, cfg.E + 1, i32),
-             mean_prob=(mean_prob, cfg.E, f32), workspace=(workspace, _size(workspace), (torch.uint8,)))
+    a, f32, T, E = _Args("rr_balance_loss"), torch.float32, cfg.T, cfg.E
+    args = (a("logits", logits, T * E, f32), a("rank_expert", rank_expert, T * (cfg.k + 1), torch.int32), a.mask(token_mask, T), coef,
+            a("loss", loss, 1, f32), a("counts", counts, E + 1, torch.int32), a("mean_prob", mean_prob, E, f32), *a.workspace(workspace))
     cc = cfg.c()
-    _check(load_library().rr_balance_loss(C.byref(cc), _ptr(logits), _ptr(rank_expert), _ptr(token_mask), coef, _ptr(loss),
-                                          _ptr(counts), _ptr(mean_prob), _ptr(workspace), _size(workspace), _stream()),
-           "rr_balance_loss")
+    _check(load_library().rr_balance_loss(C.byref(cc), *args, a.stream()), "rr_balance_loss")
 
 
 def rr_balance_loss_backward(cfg: RRConfig, logits, counts, coef: float, dlogits, dloss=None, token_mask=None,
                              accumulate: bool = False):
     """dlogits [T, E], written or (accumulate) added to; dloss [1] or None for 1."""
     import torch
-    f32 = (torch.float32,)
-    _tensors("rr_balance_loss_backward", logits=(logits, cfg.T * cfg.E, f32), counts=(counts, cfg.E + 1, (torch.int32,)),
-             token_mask=(token_mask, cfg.T, (torch.uint8, torch.bool)), dloss=(dloss, 1, f32), dlogits=(dlogits, cfg.T * cfg.E, f32))
+    a, f32, T, E = _Args("rr_balance_loss_backward"), torch.float32, cfg.T, cfg.E
+    args = (a("logits", logits, T * E, f32), a("counts", counts, E + 1, torch.int32), a.mask(token_mask, T), coef,
+            a("dloss", dloss, 1, f32), RR_GRAD_ACCUMULATE if accumulate else 0, a("dlogits", dlogits, T * E, f32))
     cc = cfg.c()
-    _check(load_library().rr_balance_loss_backward(C.byref(cc), _ptr(logits), _ptr(counts), _ptr(token_mask), coef, _ptr(dloss),
-                                                   RR_GRAD_ACCUMULATE if accumulate else 0, _ptr(dlogits), _stream()),
-           "rr_balance_loss_backward")
+    _check(load_library().rr_balance_loss_backward(C.byref(cc), *args, a.stream()), "rr_balance_loss_backward")
 
 
-def _dropout_type(x):
+def _dropout_type(t):
     import torch
-    if x.dtype not in (torch.float32, torch.bfloat16):
-        raise RRError(f"dropout: unsupported type {x.dtype}")
-    return RR_F32 if x.dtype == torch.float32 else RR_BF16
+    dtype = t.dtype
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise RRError(f"dropout: unsupported type {dtype}")
+    return RR_F32 if dtype is torch.float32 else RR_BF16
 
 
 def rr_dropout(x, p: float, seed: int, offset: int, out, residual=None, device_offset=None):
     """out = residual + dropout(x), any shape; out may be x or residual.  device_offset: None or one int64 on the GPU, added to
     `offset` when the kernel runs (captured graphs).  A call uses up (x.numel() + 7) // 8 counters from `offset` on."""
     import torch
-    dtype, n = _dropout_type(x), x.numel()
-    _tensors("rr_dropout", x=(x, n, (x.dtype,)), residual=(residual, n, (x.dtype,)), out=(out, n, (x.dtype,)),
-             device_offset=(device_offset, 1, (torch.int64,)))
-    _check(load_library().rr_dropout(n, dtype, _ptr(x), _ptr(residual), p, seed, offset, _ptr(device_offset), _ptr(out), _stream()),
-           "rr_dropout")
+    a, dtype, n, t = _Args("rr_dropout"), _dropout_type(x), x.numel(), x.dtype
+    _check(load_library().rr_dropout(n, dtype, a("x", x, n, t), a("residual", residual, n, t), p, seed, offset,
+                                     a("device_offset", device_offset, 1, torch.int64), a("out", out, n, t), a.stream()), "rr_dropout")
 
 
 def rr_dropout_backward(dout, p: float, seed: int, offset: int, dx, device_offset=None):
     """dx from dout with the mask of the forward call of the same p, seed and offset; dx may be dout."""
     import torch
-    dtype, n = _dropout_type(dout), dout.numel()
-    _tensors("rr_dropout_backward", dout=(dout, n, (dout.dtype,)), dx=(dx, n, (dout.dtype,)),
-             device_offset=(device_offset, 1, (torch.int64,)))
-    _check(load_library().rr_dropout_backward(n, dtype, _ptr(dout), p, seed, offset, _ptr(device_offset), _ptr(dx), _stream()),
+    a, dtype, n, t = _Args("rr_dropout_backward"), _dropout_type(dout), dout.numel(), dout.dtype
+    _check(load_library().rr_dropout_backward(n, dtype, a("dout", dout, n, t), p, seed, offset,
+                                              a("device_offset", device_offset, 1, torch.int64), a("dx", dx, n, t), a.stream()),
            "rr_dropout_backward")
 
 
@@ -359,25 +382,21 @@ def alloc_linear_workspace(cfg: RRLinearConfig, backward: bool = False, device="
 def rr_linear(cfg: RRLinearConfig, x, w, bias, residual, y, pre, workspace):
     """y = residual + act(x W^T + bias); bias, residual and pre (the pre-activations, an output) may be None."""
     import torch
-    t, f32 = _torch_type(cfg.dtype), (torch.float32,)
-    _tensors("rr_linear", x=(x, cfg.M * cfg.K, t), w=(w, cfg.rows * cfg.K, t), bias=(bias, cfg.rows, f32),
-             residual=(residual, cfg.M * cfg.N, t), y=(y, cfg.M * cfg.N, t), pre=(pre, cfg.M * cfg.rows, t),
-             workspace=(workspace, _size(workspace), (torch.uint8,)))
+    a, t, M, N, R = _Args("rr_linear"), _torch_type(cfg.dtype), cfg.M, cfg.N, cfg.rows
+    args = (a("x", x, M * cfg.K, t), a("w", w, R * cfg.K, t), a("bias", bias, R, torch.float32), a("residual", residual, M * N, t),
+            a("y", y, M * N, t), a("pre", pre, M * R, t), *a.workspace(workspace))
     cc = cfg.c()
-    _check(load_library().rr_linear(C.byref(cc), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y), _ptr(pre), _ptr(workspace),
-                                    _size(workspace), _stream()), "rr_linear")
+    _check(load_library().rr_linear(C.byref(cc), *args, a.stream()), "rr_linear")
 
 
 def rr_linear_backward(cfg: RRLinearConfig, x, w, pre, dy, dx, dw, dbias, workspace):
     """dx, dw and dbias (None: not wanted) from dy and the pre-activations of the forward call (None without an activation)."""
     import torch
-    t, f32 = _torch_type(cfg.dtype), (torch.float32,)
-    _tensors("rr_linear_backward", x=(x, cfg.M * cfg.K, t), w=(w, cfg.rows * cfg.K, t), pre=(pre, cfg.M * cfg.rows, t),
-             dy=(dy, cfg.M * cfg.N, t), dx=(dx, cfg.M * cfg.K, t), dw=(dw, cfg.rows * cfg.K, t), dbias=(dbias, cfg.rows, f32),
-             workspace=(workspace, _size(workspace), (torch.uint8,)))
+    a, t, M, K, N, R = _Args("rr_linear_backward"), _torch_type(cfg.dtype), cfg.M, cfg.K, cfg.N, cfg.rows
+    args = (a("x", x, M * K, t), a("w", w, R * K, t), a("pre", pre, M * R, t), a("dy", dy, M * N, t), a("dx", dx, M * K, t),
+            a("dw", dw, R * K, t), a("dbias", dbias, R, torch.float32), *a.workspace(workspace))
     cc = cfg.c()
-    _check(load_library().rr_linear_backward(C.byref(cc), _ptr(x), _ptr(w), _ptr(pre), _ptr(dy), _ptr(dx), _ptr(dw), _ptr(dbias),
-                                             _ptr(workspace), _size(workspace), _stream()), "rr_linear_backward")
+    _check(load_library().rr_linear_backward(C.byref(cc), *args, a.stream()), "rr_linear_backward")
 
 
 def rr_profile_enable(on: bool):

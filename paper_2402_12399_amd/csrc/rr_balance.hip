@@ -7,20 +7,23 @@
 // for them; one record per workgroup (sums, counts, n) is added up in a fixed order by balance_finish, or by the workgroup
 // itself where there is only one.  The gradient needs f, so it is a second pass over the scores: the probabilities are made
 // again rather than stored.
+// Bound by HBM and, a little below it, by the instructions of exponentials and reductions.  2^20 tokens, 64 experts, top-2: loss
+// 55 us + 6 (281 MB, 4.6 TB/s; with expf, shuffles through LDS, a lane per row for the choices and one row at a time 135 + 30),
+// gradient 86 us (537 MB, 6.2 TB/s).  1001 tokens, 16 experts: 6.4 and 3.6 us, one workgroup without records.
 #include "rr_device.h"
 
 namespace rr {
 
 namespace {
 
-constexpr int BL_THREADS = 256;
-constexpr int BL_MAX_BLOCKS = 1024;  // records that balance_finish adds up
+constexpr int BL_THREADS = 1024, BL_MAX_BLOCKS = 256;  // the loss: few workgroups, so that few records are left
+constexpr int BG_THREADS = 256;
+constexpr int BL_UNROLL = 4;  // rows that a lane loads before it needs the first
 
-// What a workgroup leaves: probabilities summed, choices and tokens counted.
-struct BalanceRecord {
-  double prob[kMaxE];
-  int32_t count[kMaxE];
-  int32_t tokens, pad[31];
+// What a workgroup leaves: probabilities summed, choices (and, in the last column, tokens) counted.
+struct BalanceRecords {
+  double prob[BL_MAX_BLOCKS][kMaxE];
+  int32_t count[BL_MAX_BLOCKS][kMaxE + 1];
 };
 
 struct BalanceArgs {
@@ -32,7 +35,7 @@ struct BalanceArgs {
   float *loss;
   int32_t *counts;
   float *mean_prob;
-  BalanceRecord *records;
+  BalanceRecords *records;
 };
 
 // The four experts of a lane: in a row (VEC: the row is read 16 bytes at a time) or LANES apart.
@@ -54,17 +57,34 @@ __device__ inline void load_row(const float *row, int E, int lane, float (&a)[4]
     }
   }
 }
+// Reductions over the lanes of a row, by DPP: neighbours, pairs, then mirrored halves of 8 and of 16 lanes.
+template <int CTRL>
+__device__ inline float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
 template <int LANES>
 __device__ inline float row_max(float v) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  if (LANES >= 2) v = fmaxf(v, dpp<0xB1>(v));
+  if (LANES >= 4) v = fmaxf(v, dpp<0x4E>(v));
+  if (LANES >= 8) v = fmaxf(v, dpp<0x141>(v));
+  if (LANES >= 16) v = fmaxf(v, dpp<0x140>(v));
   return v;
 }
 template <int LANES>
 __device__ inline float row_sum(float v) {
-#pragma unroll
-  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if (LANES >= 2) v += dpp<0xB1>(v);
+  if (LANES >= 4) v += dpp<0x4E>(v);
+  if (LANES >= 8) v += dpp<0x141>(v);
+  if (LANES >= 16) v += dpp<0x140>(v);
   return v;
+}
+// exp(x) for x <= 0 to 2 u: 2^t with t the rounded x / ln 2, times 1 + ln 2 (x / ln 2 - t); 0 where it is below 2^-126, and for
+// -infinity.  (Half of expf's instructions, which bind the loss.)
+__device__ inline float exp_short(float x) {
+  constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = (float)(1.44269504088896341 - (double)kLog2e), kLn2 = 0.69314718055994531f;
+  x = x < -104.0f ? -104.0f : x;  // (NaN stays)
+  const float t = x * kLog2e, r = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e * r, kLn2, e);
 }
 // Scores -> unnormalised probabilities; returns 1 / their sum (0 for a row of -infinity only).
 template <int LANES>
@@ -72,9 +92,10 @@ __device__ inline float softmax_row(float (&a)[4]) {
   const float m = row_max<LANES>(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])));
   const float top = m == -INFINITY ? 0.0f : m;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) a[j] = expf(a[j] - top);
-  const float sum = row_sum<LANES>(a[0] + a[1] + a[2] + a[3]);
-  return sum == 0.0f ? 0.0f : 1.0f / sum;
+  for (int j = 0; j < 4; ++j) a[j] = exp_short(a[j] - top);
+  const float sum = row_sum<LANES>((a[0] + a[1]) + (a[2] + a[3]));
+  const float r = __builtin_amdgcn_rcpf(sum);  // 1 ulp; a step of Newton's makes it half of one
+  return sum == 0.0f ? 0.0f : fmaf(fmaf(-sum, r, 1.0f), r, r);
 }
 
 // One thread per expert, the first wave: loss and the outputs from the sums.
@@ -97,32 +118,43 @@ __device__ inline void write_balance(const BalanceArgs &A, double prob, int coun
 
 template <int LANES, bool VEC>
 __global__ __launch_bounds__(BL_THREADS) void balance_loss_kernel(BalanceArgs A) {
-  constexpr int ROWS = kWave / LANES, WAVES = BL_THREADS / kWave;
+  constexpr int ROWS = kWave / LANES, WAVES = BL_THREADS / kWave, U = BL_UNROLL, STEP = ROWS * U;
   __shared__ double sums[WAVES][kMaxE];
-  __shared__ int32_t hist[kMaxE];
-  __shared__ int32_t live_tokens;
+  __shared__ int32_t hist[kMaxE + 1];  // the last one: tokens
   const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid >> 6, E = A.E, k = A.k;
-  if (tid < kMaxE) hist[tid] = 0;
-  if (tid == 0) live_tokens = 0;
+  if (tid <= kMaxE) hist[tid] = 0;
   __syncthreads();
   double prob[4] = {0.0, 0.0, 0.0, 0.0};
   int live = 0;
-  const int step = gridDim.x * WAVES * ROWS;
-  for (int t0 = (blockIdx.x * WAVES + w) * ROWS; t0 < A.T; t0 += step) {
-    const int t = t0 + lane / LANES;
-    const bool counted = t < A.T && (!A.mask || A.mask[t]);
-    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (counted) load_row<LANES, VEC>(A.logits + (size_t)t * E, E, lane, a);
-    const float inv = softmax_row<LANES>(a);
-    if (counted) {
+  const long long step = (long long)gridDim.x * WAVES * STEP;
+  for (long long t0 = ((long long)blockIdx.x * WAVES + w) * STEP; t0 < A.T; t0 += step) {
+    float a[U][4];
+    bool counted[U];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) prob[j] += (double)(a[j] * inv);
-      if ((lane & (LANES - 1)) == 0) {
+    for (int u = 0; u < U; ++u) {
+      const long long t = t0 + u * ROWS + lane / LANES;
+      counted[u] = t < A.T && (!A.mask || A.mask[t]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) a[u][j] = 0.0f;
+      if (counted[u]) load_row<LANES, VEC>(A.logits + (size_t)t * E, E, lane, a[u]);
+    }
+    // the choices of these rows: lane l looks at choice l % 4 of every 16th row
+#pragma unroll
+    for (int i = 0; i < STEP; i += kWave / kMaxK) {
+      const long long t = t0 + i + (lane >> 2);
+      const int r = lane & 3;
+      if (i + (lane >> 2) < STEP && r < k && t < A.T && (!A.mask || A.mask[t])) {
+        const int e = A.rank_expert[(size_t)t * (k + 1) + r];
+        if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float inv = softmax_row<LANES>(a[u]);
+      if (counted[u]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) prob[j] += (double)(a[u][j] * inv);
         ++live;
-        for (int r = 0; r < k; ++r) {
-          const int e = A.rank_expert[(size_t)t * (k + 1) + r];
-          if (e >= 0 && e < E) atomicAdd(&hist[e], 1);
-        }
       }
     }
   }
@@ -132,9 +164,8 @@ __global__ __launch_bounds__(BL_THREADS) void balance_loss_kernel(BalanceArgs A)
     for (int j = 0; j < 4; ++j) prob[j] += __shfl_xor(prob[j], o);
   if (lane < LANES)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (expert_of<LANES, VEC>(lane, j) < kMaxE) sums[w][expert_of<LANES, VEC>(lane, j)] = prob[j];
-  if (live) atomicAdd(&live_tokens, live);
+    for (int j = 0; j < 4; ++j) sums[w][expert_of<LANES, VEC>(lane, j)] = prob[j];
+  if ((lane & (LANES - 1)) == 0 && live) atomicAdd(&hist[kMaxE], live);
   __syncthreads();
   if (tid >= kWave) return;
   double total = 0.0;
@@ -142,27 +173,40 @@ __global__ __launch_bounds__(BL_THREADS) void balance_loss_kernel(BalanceArgs A)
 #pragma unroll
     for (int q = 0; q < WAVES; ++q) total += sums[q][tid];
   if (gridDim.x == 1) {
-    write_balance(A, total, hist[tid], live_tokens);
+    write_balance(A, total, hist[tid], hist[kMaxE]);
     return;
   }
-  BalanceRecord &R = A.records[blockIdx.x];
-  R.prob[tid] = total;
-  R.count[tid] = hist[tid];
-  if (tid == 0) R.tokens = live_tokens;
+  A.records->prob[blockIdx.x][tid] = total;
+  A.records->count[blockIdx.x][tid] = hist[tid];
+  if (tid == 0) A.records->count[blockIdx.x][kMaxE] = hist[kMaxE];
 }
 
-// Adds up the records: thread (part, expert) every 16th record, then the parts in order.
+// Adds up the records of n workgroups: thread (part, expert) takes every 16th of them, a batch of loads at a time, then the
+// parts are added in order.
 __global__ __launch_bounds__(1024) void balance_finish_kernel(BalanceArgs A, int n) {
-  constexpr int PARTS = 1024 / kWave;
+  constexpr int PARTS = 1024 / kWave, BATCH = 16;
   __shared__ double sums[PARTS][kMaxE];
   __shared__ int32_t hist[PARTS][kMaxE], tokens[PARTS];
   const int e = threadIdx.x & (kWave - 1), part = threadIdx.x >> 6;
   double prob = 0.0;
   int count = 0, live = 0;
-  for (int i = part; i < n; i += PARTS) {
-    prob += A.records[i].prob[e];
-    count += A.records[i].count[e];
-    live += A.records[i].tokens;
+  for (int i0 = part; i0 < n; i0 += PARTS * BATCH) {
+    double p[BATCH];
+    int c[BATCH], l[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = min(i0 + b * PARTS, n - 1);
+      p[b] = A.records->prob[i][e];
+      c[b] = A.records->count[i][e];
+      l[b] = A.records->count[i][kMaxE];
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const bool in = i0 + b * PARTS < n;
+      prob += in ? p[b] : 0.0;
+      count += in ? c[b] : 0;
+      live += in ? l[b] : 0;
+    }
   }
   sums[part][e] = prob;
   hist[part][e] = count;
@@ -186,6 +230,7 @@ __device__ inline float add(float a, float b) {
   return a + b;
 }
 
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 struct BalanceGradArgs {
   const float *logits;
   const int32_t *counts;
@@ -194,11 +239,12 @@ struct BalanceGradArgs {
   float coef;
   const float *dloss;
   float *dlogits;
+  int stream;  // store past the caches
 };
 
 template <int LANES, bool VEC, bool ADD>
-__global__ __launch_bounds__(BL_THREADS) void balance_grad_kernel(BalanceGradArgs A) {
-  constexpr int ROWS = kWave / LANES, WAVES = BL_THREADS / kWave;
+__global__ __launch_bounds__(BG_THREADS) void balance_grad_kernel(BalanceGradArgs A) {
+  constexpr int ROWS = kWave / LANES, WAVES = BG_THREADS / kWave;
   const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x >> 6, E = A.E;
   const int n = A.counts[E];
   const float each = n > 0 ? 1.0f / ((float)A.k * (float)n) : 0.0f;
@@ -209,10 +255,11 @@ __global__ __launch_bounds__(BL_THREADS) void balance_grad_kernel(BalanceGradArg
     const int e = expert_of<LANES, VEC>(lane, j);
     f[j] = e < E ? (float)A.counts[e] * each : 0.0f;
   }
+  // from the last row to the first: the loss has just read the last ones, which the last-level cache still holds
   const int step = gridDim.x * WAVES * ROWS;
   for (int t0 = (blockIdx.x * WAVES + w) * ROWS; t0 < A.T; t0 += step) {
-    const int t = t0 + lane / LANES;
-    const bool in = t < A.T, counted = in && (!A.mask || A.mask[t]);
+    const int t = A.T - 1 - t0 - lane / LANES;
+    const bool in = t >= 0, counted = in && (!A.mask || A.mask[t]);
     float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (counted) load_row<LANES, VEC>(A.logits + (size_t)t * E, E, lane, a);
     const float inv = softmax_row<LANES>(a);
@@ -228,6 +275,7 @@ __global__ __launch_bounds__(BL_THREADS) void balance_grad_kernel(BalanceGradArg
         float4 *at = reinterpret_cast<float4 *>(row + e);
         const float4 v = ADD ? *at : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (ADD) *at = make_float4(add(v.x, g[0]), add(v.y, g[1]), add(v.z, g[2]), add(v.w, g[3]));
+        else if (A.stream) __builtin_nontemporal_store(f32x4_t{g[0], g[1], g[2], g[3]}, reinterpret_cast<f32x4_t *>(at));
         else *at = make_float4(g[0], g[1], g[2], g[3]);
       }
     } else {
@@ -240,9 +288,8 @@ __global__ __launch_bounds__(BL_THREADS) void balance_grad_kernel(BalanceGradArg
   }
 }
 
-// Workgroups for T rows, ROWS a wave.
-int balance_blocks(int T, int lanes, int most) {
-  const int rows = kWave / lanes * (BL_THREADS / kWave);
+// Workgroups that take `rows` rows each at a time.
+int balance_blocks(int T, int rows, int most) {
   const int blocks = (T + rows - 1) / rows;
   return blocks < most ? blocks : most;
 }
@@ -265,16 +312,17 @@ void with_lanes(int E, bool vec, F f) {
 
 }  // namespace
 
-size_t balance_workspace() { return sizeof(BalanceRecord) * BL_MAX_BLOCKS; }
+size_t balance_workspace() { return (sizeof(BalanceRecords) + 255) / 256 * 256; }
 
 hipError_t launch_balance_loss(int T, int E, int k, const float *logits, const int32_t *rank_expert, const uint8_t *mask, float coef,
                                float *loss, int32_t *counts, float *mean_prob, void *ws, hipStream_t s) {
-  const BalanceArgs A{logits, rank_expert, mask, T, E, k, coef, loss, counts, mean_prob, static_cast<BalanceRecord *>(ws)};
+  const BalanceArgs A{logits, rank_expert, mask, T, E, k, coef, loss, counts, mean_prob, static_cast<BalanceRecords *>(ws)};
   int blocks = 1;
   prof_begin(K_BALANCE, s);
   with_lanes(E, E % 4 == 0 && aligned(logits), [&](auto lanes, auto vec) {
     constexpr int LANES = decltype(lanes)::value;
-    blocks = balance_blocks(T, LANES, BL_MAX_BLOCKS);
+    constexpr int rows = kWave / LANES * BL_UNROLL * (BL_THREADS / kWave);
+    blocks = T <= 4 * rows ? 1 : balance_blocks(T, rows, BL_MAX_BLOCKS);
     balance_loss_kernel<LANES, decltype(vec)::value><<<blocks, BL_THREADS, 0, s>>>(A);
   });
   if (blocks > 1) balance_finish_kernel<<<1, 1024, 0, s>>>(A, blocks);
@@ -284,14 +332,18 @@ hipError_t launch_balance_loss(int T, int E, int k, const float *logits, const i
 
 hipError_t launch_balance_grad(int T, int E, int k, const float *logits, const int32_t *counts, const uint8_t *mask, float coef,
                                const float *dloss, bool add, float *dlogits, hipStream_t s) {
-  const BalanceGradArgs A{logits, counts, mask, T, E, k, coef, dloss, dlogits};
+  // Scores and gradient that the last-level cache does not hold together: the gradient goes past it, or its dirty lines are what
+  // the next pass over the scores waits for.  2^20 tokens, 64 experts: loss 79 -> 55 us, gradient 88 -> 86 (without the order
+  // of rows below: 94).  Smaller ones stay there for who reads them next.
+  constexpr size_t kLastLevelBytes = (size_t)256 << 20;
+  const BalanceGradArgs A{logits, counts, mask, T, E, k, coef, dloss, dlogits, 2 * (size_t)T * E * 4 > kLastLevelBytes};
   prof_begin(K_BALANCE_BWD, s);
   with_lanes(E, E % 4 == 0 && aligned(logits) && aligned(dlogits), [&](auto lanes, auto vec) {
     constexpr int LANES = decltype(lanes)::value;
     constexpr bool VEC = decltype(vec)::value;
-    const int blocks = balance_blocks(T, LANES, 1 << 14);
-    if (add) balance_grad_kernel<LANES, VEC, true><<<blocks, BL_THREADS, 0, s>>>(A);
-    else balance_grad_kernel<LANES, VEC, false><<<blocks, BL_THREADS, 0, s>>>(A);
+    const int blocks = balance_blocks(T, kWave / LANES * (BG_THREADS / kWave), 1 << 14);
+    if (add) balance_grad_kernel<LANES, VEC, true><<<blocks, BG_THREADS, 0, s>>>(A);
+    else balance_grad_kernel<LANES, VEC, false><<<blocks, BG_THREADS, 0, s>>>(A);
   });
   prof_end(K_BALANCE_BWD, s);
   return hipGetLastError();

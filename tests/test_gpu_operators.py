@@ -131,7 +131,8 @@ def balance_bounds(want, logits, coef, dloss):
     """With s the widest span of a row's scores: a probability's exponent is off by at most u s (the difference's rounding), the
     exponential, the sum over up to 64 experts (8 levels), the reciprocal and the product by 16 u more, and so is the sum it is
     divided by: c = (2 s + 20) u relative.  The gradient p (f - mean) takes f from two more roundings and the mean from sums
-    of f p of 8 levels."""
+    of f p of 8 levels.  An exponential below t = 2^-126, the smallest normal number, is taken for 0: p, at most the
+    exponential because the sum is at least 1, is then off by t, P_e too, the loss by coef E t, the gradient by 2 scale t."""
     finite = logits[torch.isfinite(logits)]
     s = float((finite.max() - finite.min())) if finite.numel() else 0.0
     c = (2 * s + 20) * U
@@ -140,7 +141,9 @@ def balance_bounds(want, logits, coef, dloss):
     n = max(int(want["counts"][-1]), 1)
     scale = abs(dloss * coef) * E / n
     grad = scale * want["p"] * ((c + 8 * U) * (want["f"] + pf) + c * (want["f"] - pf).abs() + (c + 12 * U) * pf)
-    return c * want["mean_prob"] + 1e-40, (c + 4 * U) * float(want["loss"].abs()) + 1e-40, grad + 1e-40
+    t = 2.0 ** -126
+    return (c * want["mean_prob"] + t + 1e-40, (c + 4 * U) * float(want["loss"].abs()) + abs(coef) * E * t + 1e-40,
+            grad + 2 * scale * t + 1e-40)
 
 
 def run_balance(a, ranks, k, coef, mask=None, dloss=None, accumulate=None):
