@@ -460,6 +460,13 @@ int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, siz
   return rc;
 }
 
+// Host function for tests: see LinearPlans.
+int rr_linear_plans(const rr_linear_config *cfg, LinearPlans *out) {
+  const int rc = check_linear(cfg);
+  if (rc == RR_OK) linear_describe(*cfg, out);
+  return rc;
+}
+
 int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual, void *y, void *pre,
               void *workspace, size_t workspace_bytes, void *stream) {
   const int rc = check_linear(cfg);

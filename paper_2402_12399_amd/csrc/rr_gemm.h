@@ -57,16 +57,17 @@ __device__ __forceinline__ void sched_mfma_lds_read() {
 // the source: they write LDS, so the compiler moves no LDS read across them, and groups that ask for a load between two
 // reads are not followed at all (the reads then run in one burst; 16384 tokens x 4096 x 11008: gate/up 4.66 -> 4.50 ms,
 // down 2.34 -> 2.24, the MFMA pipe's share of the busy cycles 0.71 -> 0.77, the clock 1.75 -> 1.71 GHz).
-template <int M, int R, int D>
+// P: LDS reads behind one MFMA (turned operands take two reads per fragment).
+template <int M, int R, int D, int P = 1>
 __device__ __forceinline__ void sched_step() {
   if constexpr (M > 0 && R > 0) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    sched_step<M - 1, R - 1, D>();
+    __builtin_amdgcn_sched_group_barrier(0x100, R < P ? R : P, 0);
+    sched_step<M - 1, (R < P ? 0 : R - P), D, P>();
   } else if constexpr (M > 0 && D > 0) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
-    sched_step<M - 1, 0, D - 1>();
+    sched_step<M - 1, 0, D - 1, P>();
   }
 }
 
@@ -111,8 +112,9 @@ struct GemmArgs {
 // summation, whose raw sums go to `part` when there are several.
 struct DenseArgs : GemmArgs {  // K: elements of a slice
   int M, MT;             // rows, row tiles
-  int slices, LD;        // LD: elements between rows, of A and B alike
-  int Kall;              // elements of a row
+  int slices;
+  int lda, ldb;          // elements between rows of A and of B (turned operands: of their memory); gemm_tile_kernel: the same
+  int Kall;              // elements of the whole summation
   const float *bias;     // [R], R = N, gated 2 N (B1 = B0 + N rows); or NULL
   const void *residual;  // [M, N] or NULL
   void *pre;             // [M, R] or NULL
@@ -288,13 +290,38 @@ constexpr int PK_SMEM = PK_B_BASE + PK_B_STAGES * PK_B_STAGE;  // 160 KB: all of
 [[maybe_unused]] constexpr int PK_NI = (PK_BM + PK_BROWS) / 8 / PK_NW;  // 1 KB load instructions per wave per chunk
 [[maybe_unused]] constexpr int PK_NIA = PK_BM / 8 / PK_NW;
 
-template <bool GATED, int ACT, bool GATHER, bool DIRECT = false, bool DENSE = false>
+// Turned operands (TA, TB; dense products): the summation runs down the memory's rows, as in dx = dz W and dw = dz^T x.  A chunk
+// is then 64 memory rows of 256 neighbouring columns, 512 bytes each, staged as they lie (a DMA instruction fills two), and the
+// fragments come out of LDS through ds_read_b64_tr_b16: 16 lanes name the 4 pieces of 8 bytes of each of 4 rows, and lane l gets
+// column l of the four.  A lane's eight elements are two such reads, rows 8 g .. + 3 and + 4 .. + 7 (g = lane / 16), as in an
+// operand that is not turned.  32-byte unit c of row k sits at c ^ turn_swz(k): the eight rows that 32 lanes read at once
+// then lie in different eighths of the 64 banks.  Rows past the end of the summation read as zero (range check), columns past the
+// operand's edge hold the next row's and are not stored.
+__device__ inline int turn_swz(int k) { return (k & 3) | (k >> 1 & 4); }
+constexpr int TR_ROW_BYTES = 512;
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+// A turned fragment of 32 x 16 elements whose first row of this lane is at `at` in LDS.  (__restrict__ is not about aliases here: it
+// leaves a scope on the reads, without which the compiler takes them for possible readers of every DMA load under way and drains
+// those, vmcnt(0), before each group of reads.)
+__device__ __forceinline__ bf16x8 read_turned(const char *__restrict__ at) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)at);
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(at + 4 * TR_ROW_BYTES));
+  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#else
+  return bf16x8{};
+#endif
+}
+
+template <bool GATED, int ACT, bool GATHER, bool DIRECT = false, bool DENSE = false, bool TA = false, bool TB = false>
 __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typename std::conditional<DENSE, DenseArgs, GemmArgs>::type P) {
 #if defined(__HIP_DEVICE_COMPILE__)  // buffer-resource and LDS-DMA builtins exist in the device pass only
   constexpr int WM = PK_WM, WN = PK_WN, NW = PK_NW, BM = PK_BM, NI = PK_NI, NIA = PK_NIA;
   constexpr int BN = GATED ? PK_BROWS / 2 : PK_BROWS;
   constexpr int NIB0 = BN / 8 / NW;
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "operand boundaries must fall between load instructions");
+  static_assert(!(TA || TB) || (DENSE && !GATED && !GATHER));
   extern __shared__ __attribute__((aligned(16))) char smem[];
 
   const int K = P.K, N = P.N, NT = P.NT, KT = (K + GB_BK - 1) / GB_BK;
@@ -352,6 +379,15 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
   const int a_off = (wm * 16 + fr) * GB_ROW_BYTES;  // fragment i: + i * PK_WAVES_M * 16 rows
   // gated: the first half of a wave's column fragments are gate columns, the second the matching up columns
   const int b_off = (wn * (GATED ? WN / 2 : WN) * 16 + fr) * GB_ROW_BYTES;
+  // turned operands: the lane's offset for fragment i (A: i % 4; the others are 256 bytes further), first row
+  int a_turn[4], b_turn[WN];
+  if constexpr (TA || TB) {
+    const int k = 8 * fg + (fr >> 2), f = turn_swz(k), at = k * TR_ROW_BYTES + (fr & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a_turn[i] = at + ((i * PK_WAVES_M + wm) ^ f) * 32;
+#pragma unroll
+    for (int j = 0; j < WN; ++j) b_turn[j] = at + ((wn * WN + j) ^ f) * 32;
+  }
   auto b_frag = [&](int j) { return (GATED && j >= WN / 2 ? BN + (j - WN / 2) * 16 : j * 16) * GB_ROW_BYTES; };
 
   // per-tile state.  A tile's table entry is fetched two tiles ahead and (GATHER) its token indices
@@ -384,9 +420,15 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
   };
   const int lrow = w * 8 + (lane >> 3);            // stage row of this lane in instruction 0
   const int lcol = ((lane & 7) ^ swz(lrow)) * 16;  // byte position of its 16-byte chunk in the global row
-  int LD = K;
-  if constexpr (DENSE) LD = P.LD;
-  const unsigned rstep = NW * 8 * LD * 2;           // bytes between the rows of consecutive instructions
+  int lda = K, ldb = K;
+  if constexpr (DENSE) {
+    lda = P.lda;
+    ldb = P.ldb;
+  }
+  // bytes between the rows of consecutive instructions
+  const unsigned rstep = NW * (TA ? 2 : 8) * lda * 2, rstep_b = NW * (TB ? 2 : 8) * ldb * 2;
+  const int trow = w * 2 + (lane >> 5), tcol = ((lane & 31) ^ turn_swz(trow) << 1) * 16;  // turned: as lrow and lcol
+  static_assert(NW * 2 % 16 == 0, "the swizzle of a turned operand must not depend on the instruction index");
   // this lane's piece of the last chunk lies past the end of the row (K no multiple of the chunk)
   const bool past = (KT - 1) * GB_BK * 2 + lcol >= K * 2;
   const char *Ab = static_cast<const char *>(P.A);
@@ -436,15 +478,16 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
   auto make_tile = [&](const Info &f, const int (&tok)[NIA], Tile &t) {
     t.e = f.e; t.m0 = f.m0; t.rbase = f.rbase; t.rows_e = f.rows_e; t.n0 = f.n0;
     t.live = (min(BM, f.rows_e - f.m0) + PK_WAVES_M * 16 - 1) / (PK_WAVES_M * 16);
-    if constexpr (DENSE) {  // operands that start at the tile's first row and the slice's first element
-      const size_t k0 = (size_t)f.e * K * 2, pitch = (size_t)LD * 2;
-      t.pa = reinterpret_cast<unsigned long long>(Ab + f.m0 * pitch + k0);
-      t.na = (int)(min(BM, f.rows_e - f.m0) * pitch - k0);
-      t.pb0 = reinterpret_cast<unsigned long long>(static_cast<const char *>(P.B0) + f.n0 * pitch + k0);
-      t.pb1 = GATED ? reinterpret_cast<unsigned long long>(static_cast<const char *>(P.B1) + f.n0 * pitch + k0) : t.pb0;
-      t.nb = (int)(min(BN, N - f.n0) * pitch - k0);
-      t.va[0] = lrow * LD * 2 + lcol;
-      t.vb = t.va[0];
+    if constexpr (DENSE) {  // operands that start at the tile's first row (turned: column) and the slice's first element
+      const size_t k0 = (size_t)f.e * K, pa = (size_t)lda * 2, pb = (size_t)ldb * 2;
+      t.pa = reinterpret_cast<unsigned long long>(Ab) + (TA ? k0 * pa + f.m0 * 2 : f.m0 * pa + k0 * 2);
+      t.pb0 = reinterpret_cast<unsigned long long>(P.B0) + (TB ? k0 * pb + f.n0 * 2 : f.n0 * pb + k0 * 2);
+      t.pb1 = GATED ? reinterpret_cast<unsigned long long>(P.B1) + f.n0 * pb + k0 * 2 : t.pb0;
+      // bytes to the operand's end; turned: memory rows of the slice
+      t.na = TA ? min(K, P.Kall - (int)k0) : (int)(min(BM, f.rows_e - f.m0) * pa - k0 * 2);
+      t.nb = TB ? min(K, P.Kall - (int)k0) : (int)(min(BN, N - f.n0) * pb - k0 * 2);
+      t.va[0] = TA ? trow * lda * 2 + tcol : lrow * lda * 2 + lcol;
+      t.vb = TB ? trow * ldb * 2 + tcol : lrow * ldb * 2 + lcol;
       return;
     }
     const char *B0b = static_cast<const char *>(P.B0) + (size_t)f.e * N * K * 2;
@@ -474,7 +517,8 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
   // last tile its ranges are 0, so that every chunk issues the same number of loads.
   constexpr int NIB = NI - NIA;
   unsigned sva[NVA], svb;  // offsets of this lane
-  int ska, skb, sna, snb;  // byte positions in K, ranges
+  int ska, skb, sna, snb;  // byte positions in K, ranges; turned: unused, memory rows left
+  int scol_a = 0, scol_b = 0;  // turned: bytes of a memory row before the tile's first column
   unsigned long long spa, spb0, spb1;
   auto stream_a = [&](const Tile &t, bool real) {
 #pragma unroll
@@ -482,6 +526,7 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
     spa = t.pa;
     sna = real ? t.na : 0;
     ska = 0;
+    if (TA) scol_a = t.m0 * 2;
   };
   auto stream_b = [&](const Tile &t, bool real) {
     svb = t.vb;
@@ -489,31 +534,46 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
     spb1 = t.pb1;
     snb = real ? (DENSE ? t.nb : N * K * 2) : 0;
     skb = 0;
+    if (TB) scol_b = t.n0 * 2;
   };
   auto issue_a = [&](int stage) {
     char *st = smem + stage * PK_A_STAGE + w * 1024;
-    const __amdgpu_buffer_rsrc_t rsA = rsrc_of(spa, sna);
+    // turned: the buffer is the chunk's memory rows, from the tile's first column on
+    const __amdgpu_buffer_rsrc_t rsA = rsrc_of(spa, TA ? max(0, min(GB_BK, sna)) * lda * 2 - (sna > 0 ? scol_a : 0) : sna);
 #pragma unroll
     for (int i = 0; i < NIA; ++i) {
       auto lp = (__attribute__((address_space(3))) void *)(st + i * NW * 1024);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsA, lp, 16, GATHER ? sva[i < NVA ? i : 0] : sva[0] + i * rstep, ska, 0, 0);
     }
-    ska += GB_BK * 2;
+    if constexpr (TA) {
+      spa += (unsigned long long)lda * (GB_BK * 2);
+      sna -= GB_BK;
+    } else {
+      ska += GB_BK * 2;
+    }
   };
   auto issue_b = [&](int stage, int i0, int i1) {  // instructions i0 .. i1 - 1 of the chunk
     char *st = smem + PK_B_BASE + stage * PK_B_STAGE + w * 1024;
-    const __amdgpu_buffer_rsrc_t rsB0 = rsrc_of(spb0, snb), rsB1 = rsrc_of(spb1, snb);
+    const int rangeb = TB ? max(0, min(GB_BK, snb)) * ldb * 2 - (snb > 0 ? scol_b : 0) : snb;
+    const __amdgpu_buffer_rsrc_t rsB0 = rsrc_of(spb0, rangeb), rsB1 = rsrc_of(spb1, rangeb);
 #pragma unroll
     for (int i = 0; i < NIB; ++i) {
       if (i < i0 || i >= i1) continue;
       // which weight matrix instruction i reads is known at compile time
       auto lp = (__attribute__((address_space(3))) void *)(st + i * NW * 1024);
       if (!GATED || i < NIB0)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsB0, lp, 16, svb + i * rstep, skb, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsB0, lp, 16, svb + i * rstep_b, skb, 0, 0);
       else
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsB1, lp, 16, svb + (i - NIB0) * rstep, skb, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsB1, lp, 16, svb + (i - NIB0) * rstep_b, skb, 0, 0);
     }
-    if (i1 == NIB) skb += GB_BK * 2;
+    if (i1 == NIB) {
+      if constexpr (TB) {
+        spb0 += (unsigned long long)ldb * (GB_BK * 2);
+        snb -= GB_BK;
+      } else {
+        skb += GB_BK * 2;
+      }
+    }
   };
   auto next_b = [](int sb) { return sb == PK_B_STAGES - 1 ? 0 : sb + 1; };
 
@@ -584,17 +644,23 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
       // A chunk is four steps: k-step ks (of two), half hf of the wave's A rows.  A step multiplies half of the
       // A fragments with all B fragments of its k-step: 16 MFMAs in a full tile.
       constexpr int HM = decltype(live_tag)::value / 2, MF = HM * WN;
+      constexpr int RA = TA ? 2 * HM : HM, RB = TB ? 2 * WN : WN, RP = TA || TB ? 2 : 1;  // LDS reads of a step
       bf16x8 af[2][HM], bfr[2][WN];
       auto load_a = [&](const char *sta, int ks, int hf) {
         const char *p = sta + a_off + (((4 * ks + fg) ^ fsw) << 4);
 #pragma unroll
         for (int i = 0; i < HM; ++i)
-          af[hf][i] = *reinterpret_cast<const bf16x8 *>(p + (hf * HM + i) * PK_WAVES_M * 16 * GB_ROW_BYTES);
+          if constexpr (TA)
+            af[hf][i] = read_turned(sta + a_turn[(hf * HM + i) & 3] + (hf * HM + i) / 4 * 256 + ks * 32 * TR_ROW_BYTES);
+          else
+            af[hf][i] = *reinterpret_cast<const bf16x8 *>(p + (hf * HM + i) * PK_WAVES_M * 16 * GB_ROW_BYTES);
       };
       auto load_b = [&](const char *stb, int ks) {
         const char *p = stb + b_off + (((4 * ks + fg) ^ fsw) << 4);
 #pragma unroll
-        for (int j = 0; j < WN; ++j) bfr[ks][j] = *reinterpret_cast<const bf16x8 *>(p + b_frag(j));
+        for (int j = 0; j < WN; ++j)
+          if constexpr (TB) bfr[ks][j] = read_turned(stb + b_turn[j] + ks * 32 * TR_ROW_BYTES);
+          else bfr[ks][j] = *reinterpret_cast<const bf16x8 *>(p + b_frag(j));
       };
       auto mfma_step = [&](int ks, int hf) {
 #pragma unroll
@@ -622,17 +688,17 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
         load_a(sta, 0, 1);
         if (DMA) issue_b(bstage, 0, NIB / 2);
         mfma_step(0, 0);
-        sched_step<MF, HM, DMA ? NIB / 2 : 0>();
+        sched_step<MF, RA, DMA ? NIB / 2 : 0, RP>();
         __builtin_amdgcn_sched_barrier(0);
         load_a(sta, 1, 0);
         load_b(stb, 1);
         if (DMA) issue_b(bstage, NIB / 2, NIB);
         mfma_step(0, 1);
-        sched_step<MF, HM + WN, DMA ? NIB - NIB / 2 : 0>();
+        sched_step<MF, RA + RB, DMA ? NIB - NIB / 2 : 0, RP>();
         __builtin_amdgcn_sched_barrier(0);
         load_a(sta, 1, 1);
         mfma_step(1, 0);
-        sched_step<MF, HM, 0>();
+        sched_step<MF, RA, 0, RP>();
         __builtin_amdgcn_sched_barrier(0);
       };
       const char *sta = smem + sa * PK_A_STAGE, *stb = smem + PK_B_BASE + sb * PK_B_STAGE;
@@ -655,8 +721,8 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
         if (kt == KT - 2) stream_b(nxt, have1);
         if (kt == KT - 1) stream_a(nxt, have1);
         if (K % GB_BK) {  // in the last chunk of a row, pieces past its end are sent out of range: they read as zero
-          if (kt == KT - 3 && past) svb = 0x7ffffff0;
-          if (kt == KT - 2 && past) {
+          if (!TB && kt == KT - 3 && past) svb = 0x7ffffff0;
+          if (!TA && kt == KT - 2 && past) {
 #pragma unroll
             for (int i = 0; i < NVA; ++i) sva[i] = 0x7ffffff0;
           }
@@ -672,7 +738,7 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
         load_b(stb, 0);
         issue_a(sa ^ 1);
         mfma_step(1, 1);  // last step of chunk kt-1
-        sched_step<MF, HM + WN, NIA>();
+        sched_step<MF, RA + RB, NIA, RP>();
         __builtin_amdgcn_sched_barrier(0);
         steps(sta, stb, std::true_type{}, next_b(next_b(sb)));
       }
@@ -809,7 +875,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     m0 = (mt - slice * P.MT) * BM;
     k0 = slice * K;
     K = min(K, P.Kall - k0);
-    LD = P.LD;
+    LD = P.lda;
   } else {
     ti = P.tiles[mt / P.sub];
     m0 = ti.row0 + mt % P.sub * BM;

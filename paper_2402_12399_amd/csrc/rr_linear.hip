@@ -2,7 +2,8 @@
 //
 // Every product is "A[rows, K] times B[N, K]^T" with K contiguous in both operands (rr_gemm.h):
 //   forward  x, W                 dx  dz, W^T                 dw  dz^T, x^T
-// The transposes are made by linear_turn_kernel, which also makes dz from dy and the stored z, and sums its columns.
+// The 256 x 256 tiles read the operands of the gradients as they lie in memory ("turned" operands); for the other tiles
+// linear_turn_kernel writes the transposes.  It also makes dz from dy and the stored z, and sums its columns.
 // Which kernel multiplies is a matter of estimated time (dense_plan): 256 x 256 tiles of the persistent kernel, smaller
 // tiles, either with the summation cut into slices where the tiles alone would leave CUs idle (each slice's raw sums go
 // to the workspace and linear_join_kernel adds them in order and does the epilogue), or, up to kFewRows rows,
@@ -267,14 +268,17 @@ struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_ke
 
 // Estimated time (us) of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
 // The numbers are the grouped GEMM's (kShape); the row tiles are known here.
-float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, int q, int slices) {
+// turned: the operands lie the other way round.  Only the 256 x 256 tiles read those as they are; for the others the time of
+// writing transposes is counted.
+enum Turned { TURNED_NONE, TURNED_B, TURNED_BOTH };
+float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, Turned turned, int q, int slices) {
   constexpr int kCUs = 256;
   const ShapeInfo &s = kShape[q];
   const int es = bf16 ? 2 : 4, ce = GB_ROW_BYTES / es, bn = gated ? s.brows / 2 : s.brows;
   const long long Ks = slices > 1 ? (K / slices + ce - 1) / ce * ce : K;
   if (slices > 1 && (Ks * slices < K || Ks * (slices - 1) >= K)) return -1.0f;
   const bool persistent = q == FFN_P256, split = q == FFN_S128 || q == FFN_S64;
-  if (persistent && (!persistent_ok((int)Ks) || (slices > 1 && Ks * slices != K))) return -1.0f;
+  if (persistent && (!persistent_ok((int)Ks) || (slices > 1 && turned != TURNED_BOTH && Ks * slices != K))) return -1.0f;
   const int KT = (int)((Ks + ce - 1) / ce);
   if (split && KT < 5) return -1.0f;
   const long long mt = (M + s.bm - 1) / s.bm, nt = (N + bn - 1) / bn, tiles = mt * nt * slices, rounds = tiles / kCUs, left = tiles - rounds * kCUs;
@@ -295,17 +299,21 @@ float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, i
   }
   float t = std::max(busy, stream) + 0.1f * busy;
   if (slices > 1) t += 4.0f + (float)part_bytes(M, R, slices) * 2.0f / kHbm;
+  if (turned != TURNED_NONE && !persistent) {
+    t += 4.0f + (float)(2 * N * K * es) / kHbm;
+    if (turned == TURNED_BOTH) t += (float)(M * K * es) / kHbm;
+  }
   return t;
 }
 
-DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated) {
+DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
   if (M <= kFewRows) return {-1, 1};
   const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : FFN_F32N;
   DensePlan best{q1, 1};
   float least = -1.0f;
   for (int q = q0; q <= q1; ++q)
     for (int s = 1; s <= kMaxSlices; ++s) {
-      const float t = dense_cost(M, N, K, bf16, gated, q, s);
+      const float t = dense_cost(M, N, K, bf16, gated, turned, q, s);
       if (t >= 0.0f && (least < 0.0f || t < least)) { least = t; best = {q, s}; }
     }
   return best;
@@ -349,10 +357,10 @@ void launch_dense_shape(int shape, const DenseArgs &A0, hipStream_t s) {
   }
 }
 
-// The product and its epilogue.  A.A, B0, B1, Cout, M, N, LD, Kall and the epilogue's pointers are set.
+// The product and its epilogue.  A.A, B0, B1, Cout, M, N, lda, ldb, Kall and the epilogue's pointers are set.  turned: only with
+// a plan of 256 x 256 tiles.
 template <bool BF16, bool GATED, int ACT>
-void launch_product(DenseArgs A, float *part, hipStream_t s) {
-  const DensePlan plan = dense_plan(A.M, A.N, A.Kall, BF16, GATED);
+void launch_product(DenseArgs A, const DensePlan &plan, Turned turned, float *part, hipStream_t s) {
   constexpr int ce = GB_ROW_BYTES / (BF16 ? 2 : 4);
   A.slices = plan.slices;
   A.K = plan.slices > 1 ? (A.Kall / plan.slices + ce - 1) / ce * ce : A.Kall;
@@ -363,16 +371,24 @@ void launch_product(DenseArgs A, float *part, hipStream_t s) {
     else linear_rows_kernel<BF16, GATED, ACT, 2><<<grid, LR_THREADS, 0, s>>>(A);
     return;
   }
-  launch_dense_shape<BF16, GATED, ACT>(plan.shape, A, s);
+  if (turned == TURNED_NONE) {
+    launch_dense_shape<BF16, GATED, ACT>(plan.shape, A, s);
+  } else if constexpr (BF16 && !GATED && ACT < 0) {
+    A.NT = (A.N + PK_BROWS - 1) / PK_BROWS;
+    A.MT = (A.M + PK_BM - 1) / PK_BM;
+    if (turned == TURNED_B) gemm_bf16_persistent_kernel<false, -1, false, false, true, false, true><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
+    else gemm_bf16_persistent_kernel<false, -1, false, false, true, true, true><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
+  }
   if (plan.slices > 1)
     linear_join_kernel<BF16, GATED, ACT><<<(unsigned)(((size_t)A.M * (A.N / 4) + 255) / 256), 256, 0, s>>>(A);
 }
 
 template <bool BF16>
 void launch_forward(int act, const DenseArgs &A, float *part, hipStream_t s) {
-  if (act == RR_ACT_SWIGLU) launch_product<BF16, true, -1>(A, part, s);
-  else if (act == RR_ACT_GELU) launch_product<BF16, false, RR_ACT_GELU>(A, part, s);
-  else launch_product<BF16, false, -1>(A, part, s);
+  const DensePlan plan = dense_plan(A.M, A.N, A.Kall, BF16, act == RR_ACT_SWIGLU, TURNED_NONE);
+  if (act == RR_ACT_SWIGLU) launch_product<BF16, true, -1>(A, plan, TURNED_NONE, part, s);
+  else if (act == RR_ACT_GELU) launch_product<BF16, false, RR_ACT_GELU>(A, plan, TURNED_NONE, part, s);
+  else launch_product<BF16, false, -1>(A, plan, TURNED_NONE, part, s);
 }
 
 template <bool BF16>
@@ -429,7 +445,21 @@ hipError_t linear_kernel_attributes() {
   set(gemm_bf16_persistent_kernel<true, -1, false, false, true>, PK_SMEM);
   set(gemm_bf16_persistent_kernel<false, RR_ACT_GELU, false, false, true>, PK_SMEM);
   set(gemm_bf16_persistent_kernel<false, -1, false, false, true>, PK_SMEM);
+  set(gemm_bf16_persistent_kernel<false, -1, false, false, true, false, true>, PK_SMEM);
+  set(gemm_bf16_persistent_kernel<false, -1, false, false, true, true, true>, PK_SMEM);
   return e;
+}
+
+void linear_describe(const rr_linear_config &c, LinearPlans *out) {
+  const bool bf16 = c.dtype == RR_BF16;
+  const int R = width(c);
+  const DensePlan plan[3] = {dense_plan(c.M, c.N, c.K, bf16, c.act == RR_ACT_SWIGLU, TURNED_NONE),
+                             dense_plan(c.M, c.K, R, bf16, false, TURNED_B), dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH)};
+  for (int i = 0; i < 3; ++i) {
+    out->bm[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].bm;
+    out->brows[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].brows;
+    out->slices[i] = plan[i].slices;
+  }
 }
 
 size_t linear_workspace(const rr_linear_config &c, bool backward) {
@@ -445,7 +475,7 @@ hipError_t launch_linear(const rr_linear_config &c, const void *x, const void *w
   A.Cout = y;
   A.M = c.M;
   A.N = c.N;
-  A.LD = A.Kall = c.K;
+  A.lda = A.ldb = A.Kall = c.K;
   A.bias = bias;
   A.residual = residual;
   A.pre = pre;
@@ -465,28 +495,37 @@ hipError_t launch_linear_backward(const rr_linear_config &c, const void *x, cons
     if (bf16) launch_turn<true>(act, A, s);
     else launch_turn<false>(act, A, s);
   };
-  auto product = [&](const void *a, const void *b, void *out, int M, int N, int K) {
+  auto product = [&](const void *a, int lda, const void *b, int ldb, void *out, int M, int N, int K, const DensePlan &plan, Turned turned) {
     DenseArgs A{};
     A.A = a;
     A.B0 = A.B1 = b;
     A.Cout = out;
     A.M = M;
     A.N = N;
-    A.LD = A.Kall = K;
-    if (bf16) launch_product<true, false, -1>(A, W.part, s);
-    else launch_product<false, false, -1>(A, W.part, s);
+    A.lda = lda;
+    A.ldb = ldb;
+    A.Kall = K;
+    if (bf16) launch_product<true, false, -1>(A, plan, turned, W.part, s);
+    else launch_product<false, false, -1>(A, plan, turned, W.part, s);
   };
   const bool act = c.act != RR_ACT_NONE;
+  const DensePlan plan_x = dense_plan(c.M, c.K, R, bf16, false, TURNED_B), plan_w = dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH);
+  const bool as_is_x = plan_x.shape == FFN_P256, as_is_w = plan_w.shape == FFN_P256;  // no transposes
+  const TurnArgs make{dy, pre, act && (dx || (dw && as_is_w)) ? W.dz : nullptr, dw && !as_is_w ? W.dz_turned : nullptr,
+                      dbias ? W.sums : nullptr, c.M, c.N, W.LT};
+  const void *dz = act ? W.dz : dy;
   prof_begin(K_LINEAR_BWD, s);
-  if (dw || dbias || (dx && act)) turn(c.act, TurnArgs{dy, pre, dx ? W.dz : nullptr, dw ? W.dz_turned : nullptr, dbias ? W.sums : nullptr, c.M, c.N, W.LT});
+  if (make.dz || make.turned || make.sums) turn(c.act, make);
   if (dbias) linear_bias_kernel<<<(R + kWave - 1) / kWave, 256, 0, s>>>(W.sums, (c.M + TN_TILE - 1) / TN_TILE, R, dbias);
   if (dx) {
-    turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
-    product(act ? W.dz : dy, W.w_turned, dx, c.M, c.K, R);
+    if (!as_is_x) turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
+    if (as_is_x) product(dz, R, w, c.K, dx, c.M, c.K, R, plan_x, TURNED_B);
+    else product(dz, R, W.w_turned, R, dx, c.M, c.K, R, plan_x, TURNED_NONE);
   }
   if (dw) {
-    turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
-    product(W.dz_turned, W.x_turned, dw, R, c.K, W.LT);
+    if (!as_is_w) turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
+    if (as_is_w) product(dz, R, x, c.K, dw, R, c.K, c.M, plan_w, TURNED_BOTH);
+    else product(W.dz_turned, W.LT, W.x_turned, W.LT, dw, R, c.K, W.LT, plan_w, TURNED_NONE);
   }
   prof_end(K_LINEAR_BWD, s);
   return hipGetLastError();

@@ -309,6 +309,34 @@ def test_linear_exact_sums(M, K, N, dtype):
         assert torch.equal(got[n], nearest(want[n], dtype) if n != "dbias" else want[n].to(F32)), n
 
 
+# 256 x 256 tiles in the forward product, in dx (W read as it lies) and in dw (dz and x read as they lie); rows and row lengths that end
+# inside a tile and inside a chunk, a last round of tiles that is cut by rows, and slices of dw
+LARGE = [(4099, 1000, 4104, "none"), (8195, 2048, 1416, "swiglu"), (2051, 4160, 4104, "gelu"), (33001, 1032, 520, "none"), (20011, 520, 1032, "swiglu")]
+
+
+@pytest.mark.parametrize("M,K,N,act", LARGE)
+def test_linear_large_tiles(M, K, N, act):
+    from tests import gpu_util as gu
+    plans = gu.linear_plans(rr.RRLinearConfig(M, K, N, rr.RR_BF16, ACT[act]))
+    print(plans)
+    x, w, b, r, R = linear_case(M, K, N, "bf16", "none", whole, M)
+    cfg = rr.RRLinearConfig(M, K, R, rr.RR_BF16, rr.RR_ACT_NONE)
+    if act == "none":
+        y, z = run_linear(x, w, b, r, "none", "bf16", N)
+        want, want_z = ref.linear(x, w, b, r, "none")
+        assert torch.equal(z, nearest(want_z, "bf16")) and torch.equal(y, nearest(want, "bf16"))
+    # the products of the gradients on whole numbers: without an activation dz is dy
+    dy = whole(gen(1), M, N, dtype=BF16)
+    want = ref.linear_backward(x, w, None, dy, "none")
+    got = run_backward(x, w, None, dy, "none", "bf16", N)
+    for n in got:
+        assert torch.equal(got[n], nearest(want[n], "bf16") if n != "dbias" else want[n].to(F32)), n
+    x[5] = float("nan")  # a row that is not finite reaches its own row and column of the gradients only
+    dy[7] = float("inf")
+    bad = run_backward(torch.nan_to_num(x), w, None, torch.nan_to_num(dy, posinf=1.0), "none", "bf16", N, ("dx",))
+    assert bool(torch.isfinite(bad["dx"]).all())
+
+
 def linear_bound(abs_sum, terms, value, dtype, slope=1.0, extra=0.0):
     """abs_sum = sum of |products|, terms of them added in fp32 in any order: every partial sum is at most abs_sum and is
     rounded once (twice in a matrix instruction): 2 u abs_sum per addition in the worst case, and at most 8 sqrt(terms) of
