@@ -24,15 +24,22 @@ __device__ inline float load_value(const void *p, size_t i) {
   return static_cast<const float *>(p)[i];
 }
 
+template <bool BF16>
+__device__ inline void store_value(void *p, size_t i, float v) {
+  if (BF16) static_cast<uint16_t *>(p)[i] = (uint16_t)pack_bf16(v, 0.0f);
+  else static_cast<float *>(p)[i] = v;
+}
+
 // ------------------------------------------------------------------ few rows
-// One to kFewRows rows: the weights are read once and everything else is small.  A workgroup owns 16 columns (gated: of both
+// Up to kFewRows rows: the weights are read once and everything else is small.  A workgroup owns 16 columns (gated: of both
 // halves of W), its waves take turns at chunks of 64 (fp32: 32) elements of the rows and load fragments straight from
 // global memory, without LDS, chunks ahead; the waves' sums are added through LDS in order.
 constexpr int kFewRows = 32;
-constexpr int LR_NW = 8, LR_THREADS = LR_NW * 64, LR_AHEAD = 4;
+constexpr int LR_NW = 8, LR_THREADS = LR_NW * 64;
+[[maybe_unused]] constexpr int LR_AHEAD = 2;
 
 template <bool BF16, bool GATED, int ACT, int MF>
-__global__ __launch_bounds__(LR_THREADS, 2) void linear_rows_kernel(DenseArgs P) {
+__global__ __launch_bounds__(LR_THREADS, 4) void linear_rows_kernel(DenseArgs P) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int ES = BF16 ? 2 : 4, NB = GATED ? 2 : 1, CHUNK = 128;  // bytes of a row
   using Frag = typename std::conditional<BF16, bf16x8, f32x4>::type;
@@ -110,8 +117,92 @@ __global__ __launch_bounds__(LR_THREADS, 2) void linear_rows_kernel(DenseArgs P)
 #endif
 }
 
+// ------------------------------------------------------------------ one to kVectorRows rows
+// As many dot products per row of W as there are rows of x: a wave takes VR rows of W (gated: VR / 2 of each half), a lane 16
+// bytes of each in every chunk of 1 KB, and the lanes' sums are added at the end.  Every wave reads whole rows, so that
+// also a narrow W is spread over the chip (16 columns a workgroup in the kernel above: 8192 -> 1024 fills 64 CUs).
+constexpr int kVectorRows = 4;
+constexpr int LV_THREADS = 256, LV_ROWS = 2;
+[[maybe_unused]] constexpr int LV_AHEAD = 4;
+
+template <bool BF16, bool GATED, int ACT, int M>
+__global__ __launch_bounds__(LV_THREADS) void linear_vector_kernel(DenseArgs P) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int ES = BF16 ? 2 : 4, PE = 16 / ES, VR = LV_ROWS;
+  constexpr int VN = GATED ? VR / 2 : VR;  // output columns of a wave
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((blockIdx.x * LV_THREADS + threadIdx.x) >> 6);
+  const int N = P.N, n0 = w * VN;
+  if (n0 >= N) return;
+  const unsigned rowb = (unsigned)P.K * ES;
+  const int chunks = (int)((rowb + 1023) / 1024);
+  const char *wrow[VR];
+#pragma unroll
+  for (int v = 0; v < VR; ++v)
+    wrow[v] = static_cast<const char *>(GATED && v >= VN ? P.B1 : P.B0) + (size_t)(n0 + v % VN) * rowb;  // N % 8 == 0: all there
+  auto rsrc = [&](const char *base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, __builtin_amdgcn_readfirstlane((int)rowb), BUF_FLAGS);
+  };
+  auto load = [](const __amdgpu_buffer_rsrc_t &rs, unsigned off) { return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0); };
+  using Quad = decltype(load(rsrc(nullptr), 0u));
+  auto value = [](const Quad &v, int i) {
+    const u32 word = v[BF16 ? i >> 1 : i];  // (a copy: __builtin_bit_cast of a vector's element takes element 0, whichever it is)
+    return __builtin_bit_cast(float, BF16 ? (i & 1 ? word & 0xffff0000u : word << 16) : word);
+  };
+  float acc[VR][M];
+#pragma unroll
+  for (int v = 0; v < VR; ++v)
+#pragma unroll
+    for (int m = 0; m < M; ++m) acc[v][m] = 0.0f;
+  // past a row's end: out of range, zero
+  for (int c0 = 0; c0 < chunks; c0 += LV_AHEAD) {
+    Quad b[LV_AHEAD][VR], a[LV_AHEAD][M];
+#pragma unroll
+    for (int s = 0; s < LV_AHEAD; ++s) {
+      const unsigned at = (unsigned)(c0 + s) * 1024 + lane * 16;
+#pragma unroll
+      for (int v = 0; v < VR; ++v) b[s][v] = load(rsrc(wrow[v]), at);
+#pragma unroll
+      for (int m = 0; m < M; ++m) a[s][m] = load(rsrc(static_cast<const char *>(P.A) + (size_t)m * rowb), at);
+    }
+#pragma unroll
+    for (int s = 0; s < LV_AHEAD; ++s)
+#pragma unroll
+      for (int i = 0; i < PE; ++i)
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+          for (int v = 0; v < VR; ++v) acc[v][m] = fmaf(value(b[s][v], i), value(a[s][m], i), acc[v][m]);
+  }
+#pragma unroll
+  for (int v = 0; v < VR; ++v)
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+      for (int o = kWave / 2; o > 0; o >>= 1) acc[v][m] += __shfl_xor(acc[v][m], o);
+  // lane m * VN + v writes column n0 + v of row m
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+#pragma unroll
+    for (int v = 0; v < VN; ++v) {
+      if (lane != m * VN + v) continue;
+      const int n = n0 + v, R = GATED ? 2 * N : N;
+      const float g = acc[v][m] + (P.bias ? P.bias[n] : 0.0f);
+      const float up = GATED ? acc[v + VR - VN][m] + (P.bias ? P.bias[N + n] : 0.0f) : 0.0f;
+      float y = GATED ? dense_silu<BF16>(g) * up : ACT == RR_ACT_GELU ? gelu_erf(g) : g;
+      if (P.pre) {
+        store_value<BF16>(P.pre, (size_t)m * R + n, g);
+        if (GATED) store_value<BF16>(P.pre, (size_t)m * R + N + n, up);
+      }
+      if (P.residual) y += load_value<BF16>(P.residual, (size_t)m * N + n);
+      store_value<BF16>(P.Cout, (size_t)m * N + n, y);
+    }
+#endif
+}
+
 // ------------------------------------------------------------------ joining slices
-// Adds the slices' sums in order and does the epilogue; a thread owns four columns (gated: of both halves).
+// Adds the slices' sums in order and does the epilogue; a thread owns four columns (gated: of both halves) and has the sums
+// of kJoinAhead slices under way.
+constexpr int kJoinAhead = 8;
 template <bool BF16, bool GATED, int ACT>
 __global__ __launch_bounds__(256) void linear_join_kernel(DenseArgs P) {
   const int N = P.N, R = GATED ? 2 * N : N, quads = N / 4;
@@ -122,8 +213,17 @@ __global__ __launch_bounds__(256) void linear_join_kernel(DenseArgs P) {
 #pragma unroll
   for (int j = 0; j < (GATED ? 2 : 1); ++j) {
     const float *at = P.part + (size_t)row * R + j * N + col;
-    acc[0][j] = *reinterpret_cast<const f32x4 *>(at);
-    for (int s = 1; s < P.slices; ++s) acc[0][j] += *reinterpret_cast<const f32x4 *>(at + (size_t)s * P.M * R);
+    acc[0][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < P.slices; s0 += kJoinAhead) {
+      f32x4 v[kJoinAhead];
+#pragma unroll
+      for (int s = 0; s < kJoinAhead; ++s) {
+        v[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (s0 + s < P.slices) v[s] = *reinterpret_cast<const f32x4 *>(at + (size_t)(s0 + s) * P.M * R);
+      }
+#pragma unroll
+      for (int s = 0; s < kJoinAhead; ++s) acc[0][j] += v[s];
+    }
   }
   DenseArgs Q = P;
   Q.part = nullptr;
@@ -266,14 +366,35 @@ size_t part_reserve(size_t M, size_t R) { return up256(std::min(part_bytes(M, R,
 
 struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_kernel
 
-// Estimated time (us) of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
-// The numbers are the grouped GEMM's (kShape); the row tiles are known here.
+// Times in us of a dense product's parts: a fit to 750 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 300 fp32
+// ones, each timed in up to 26 pairs of shape and slices.  The plan is 1.3 % (fp32: 2.2 %) off the best pair on average, 1.8 %
+// (3.0 %) on the quarter of them that the fit did not see; the worst of those by 27 % (25 %), of products of 4 us.  (The grouped GEMM's
+// numbers, which expect ragged experts and weights from HBM: 7 %, the worst by 45 %.)
+struct DenseShape { float chunk, fixed, alone; };  // as ShapeInfo: of a chunk, of a tile, of a chunk with the CU to itself (split shapes)
+struct DenseTimes {
+  int first;             // FfnShape of shape[0]
+  DenseShape shape[6];
+  float fetch, stream;   // bytes per us that a CU gets of its operands, and all of them together
+  float last, even;      // a last, partial round on top of its share; split shapes: weight of the exact number of rounds
+  float launch, join, join_slice, join_bytes;  // of any kernel; of the joining one: itself, per slice, passes over the slices' sums
+};
+constexpr DenseTimes kBf16Times{FFN_P256, {{1.345f, 0.02f}, {0.80f, 0.68f}, {0.474f, 1.07f}, {0.379f, 0.04f}, {0.267f, 0.93f}, {0.129f, 1.29f}},
+                                122e3f, 10.1e6f, 0.88f, 0.0f, 2.5f, 1.7f, 0.19f, 2.1f};
+constexpr DenseTimes kF32Times{FFN_S128, {{1.334f, 0.86f, 1.81f}, {0.734f, 0.51f, 0.81f}, {0.859f, 1.09f}, {0.501f, 0.35f}, {0.251f, 0.16f}, {0.0f, 0.0f}},
+                               57.7e3f, 4.66e6f, 0.61f, 0.27f, 3.7f, 2.2f, 0.12f, 0.91f};
+constexpr float kPersistentDense = 2.9f;  // the 256 x 256 kernel's start
+constexpr float kTurnedBoth = 1.15f;      // its K loop with both operands turned: twice the LDS reads
+constexpr float kTurnLaunch = 3.0f, kTurnBytes = 4.5e6f;
+
+// Estimated time of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
 // turned: the operands lie the other way round.  Only the 256 x 256 tiles read those as they are; for the others the time of
 // writing transposes is counted.
 enum Turned { TURNED_NONE, TURNED_B, TURNED_BOTH };
 float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, Turned turned, int q, int slices) {
   constexpr int kCUs = 256;
+  const DenseTimes &T = bf16 ? kBf16Times : kF32Times;
   const ShapeInfo &s = kShape[q];
+  const DenseShape &c = T.shape[q - T.first];
   const int es = bf16 ? 2 : 4, ce = GB_ROW_BYTES / es, bn = gated ? s.brows / 2 : s.brows;
   const long long Ks = slices > 1 ? (K / slices + ce - 1) / ce * ce : K;
   if (slices > 1 && (Ks * slices < K || Ks * (slices - 1) >= K)) return -1.0f;
@@ -282,40 +403,55 @@ float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, T
   const int KT = (int)((Ks + ce - 1) / ce);
   if (split && KT < 5) return -1.0f;
   const long long mt = (M + s.bm - 1) / s.bm, nt = (N + bn - 1) / bn, tiles = mt * nt * slices, rounds = tiles / kCUs, left = tiles - rounds * kCUs;
-  const size_t R = (size_t)N * (gated ? 2 : 1);
-  if (slices > 1 && part_bytes(M, R, slices) > kPartBytes) return -1.0f;
-  const float stream = (float)((double)(M + R) * K * es + (double)M * N * es) / kHbm;
-  const float fetch = (float)GB_ROW_BYTES * ((float)s.brows / mt + (float)s.bm / nt) / kCuFetch;
-  const float chunk = std::max(s.cost, fetch), fixed = s.fixed;
-  float busy = (float)rounds * (KT * chunk + fixed);
+  const size_t R = (size_t)N * (gated ? 2 : 1), part = part_bytes(M, R, slices);
+  if (slices > 1 && part > kPartBytes) return -1.0f;
+  const float stream = (float)((double)(M + R) * K * es + (double)M * N * es) / T.stream;
+  const float fetch = (float)GB_ROW_BYTES * ((float)s.brows / mt + (float)s.bm / nt) / T.fetch;
+  const float chunk = std::max(c.chunk * (turned == TURNED_BOTH && persistent ? kTurnedBoth : 1.0f), fetch);
+  float busy = (float)rounds * (KT * chunk + c.fixed);
   if (split) {
     const float all = (float)tiles / kCUs;
-    busy = std::max((0.56f * all + 0.44f * ceilf(all)) * (KT * chunk + fixed), KT * s.alone + fixed);
+    busy = std::max((T.even * all + (1.0f - T.even) * ceilf(all)) * (KT * chunk + c.fixed), KT * c.alone + c.fixed);
   } else if (persistent) {
-    busy += kPersistentStart;
-    if (left > 0) busy += KT * std::max(s.cost * kCutCost[std::min<long long>(kCUs / left, PK_MAX_CUT) - 1], fetch) + fixed;
+    busy += kPersistentDense;
+    if (left > 0) busy += KT * std::max(chunk * kCutCost[std::min<long long>(kCUs / left, PK_MAX_CUT) - 1], fetch) + c.fixed;
   } else if (left > 0) {
-    busy += (KT * chunk + fixed) * (rounds ? std::min(1.0f, (float)left / kCUs + 0.5f) : 1.0f);
+    busy += (KT * chunk + c.fixed) * (rounds ? std::min(1.0f, (float)left / kCUs + T.last) : 1.0f);
   }
-  float t = std::max(busy, stream) + 0.1f * busy;
-  if (slices > 1) t += 4.0f + (float)part_bytes(M, R, slices) * 2.0f / kHbm;
-  if (turned != TURNED_NONE && !persistent) {
-    t += 4.0f + (float)(2 * N * K * es) / kHbm;
-    if (turned == TURNED_BOTH) t += (float)(M * K * es) / kHbm;
-  }
+  float t = T.launch + std::max(busy, stream) + 0.1f * busy;
+  if (slices > 1) t += T.join + T.join_slice * slices + T.join_bytes * (float)part / kHbm;
+  if (turned != TURNED_NONE && !persistent)
+    t += kTurnLaunch + (float)((2 * N * K + (turned == TURNED_BOTH ? M * K : 0)) * es) / kTurnBytes;
+  return t;
+}
+
+// linear_rows_kernel: a workgroup reads its rows of W and all of A.
+float rows_cost(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
+  const DenseTimes &T = bf16 ? kBf16Times : kF32Times;
+  const int es = bf16 ? 2 : 4;
+  const long long blocks = (N + 15) / 16, bytes = ((gated ? 32 : 16) + M) * K * es;
+  constexpr float kAlone = 42.5e3f, kShared = 30.5e3f;  // bytes per us of a CU with one workgroup, with several
+  float t = T.launch + 1.1f + (float)((blocks + 255) / 256) * (float)bytes / (blocks > 256 ? kShared : kAlone);
+  if (turned != TURNED_NONE) t += kTurnLaunch + (float)((2 * N * K + (turned == TURNED_BOTH ? M * K : 0)) * es) / kTurnBytes;
   return t;
 }
 
 DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
-  if (M <= kFewRows) return {-1, 1};
+  if (M <= kVectorRows) return {-1, 1};
   const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : FFN_F32N;
   DensePlan best{q1, 1};
   float least = -1.0f;
-  for (int q = q0; q <= q1; ++q)
-    for (int s = 1; s <= kMaxSlices; ++s) {
+  if (M <= kFewRows) {
+    best = {-1, 1};
+    least = rows_cost(M, N, K, bf16, gated, turned);
+  }
+  for (int q = q0; q <= q1; ++q) {
+    const long long bn = gated ? kShape[q].brows / 2 : kShape[q].brows, tiles = (M + kShape[q].bm - 1) / kShape[q].bm * ((N + bn - 1) / bn);
+    for (int s = 1; s <= kMaxSlices && (s == 1 || tiles * s <= 2048); ++s) {  // (eight rounds: slices even nothing out any more)
       const float t = dense_cost(M, N, K, bf16, gated, turned, q, s);
       if (t >= 0.0f && (least < 0.0f || t < least)) { least = t; best = {q, s}; }
     }
+  }
   return best;
 }
 
@@ -366,6 +502,16 @@ void launch_product(DenseArgs A, const DensePlan &plan, Turned turned, float *pa
   A.K = plan.slices > 1 ? (A.Kall / plan.slices + ce - 1) / ce * ce : A.Kall;
   A.part = plan.slices > 1 ? part : nullptr;
   if (plan.shape < 0) {
+    if (A.M <= kVectorRows) {
+      const dim3 grid((A.N * (GATED ? 2 : 1) / LV_ROWS + LV_THREADS / kWave - 1) / (LV_THREADS / kWave));
+      switch (A.M) {
+        case 1: linear_vector_kernel<BF16, GATED, ACT, 1><<<grid, LV_THREADS, 0, s>>>(A); break;
+        case 2: linear_vector_kernel<BF16, GATED, ACT, 2><<<grid, LV_THREADS, 0, s>>>(A); break;
+        case 3: linear_vector_kernel<BF16, GATED, ACT, 3><<<grid, LV_THREADS, 0, s>>>(A); break;
+        default: linear_vector_kernel<BF16, GATED, ACT, 4><<<grid, LV_THREADS, 0, s>>>(A); break;
+      }
+      return;
+    }
     const dim3 grid((A.N + 15) / 16);
     if (A.M <= 16) linear_rows_kernel<BF16, GATED, ACT, 1><<<grid, LR_THREADS, 0, s>>>(A);
     else linear_rows_kernel<BF16, GATED, ACT, 2><<<grid, LR_THREADS, 0, s>>>(A);
