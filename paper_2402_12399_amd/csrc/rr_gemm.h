@@ -53,6 +53,15 @@ __device__ __forceinline__ void sched_mfma_lds_read() {
     sched_mfma_lds_read<N - 1>();
   }
 }
+// As many pairs of reads (turned operands):
+template <int N>
+__device__ __forceinline__ void sched_mfma_two_lds_reads() {
+  if constexpr (N > 0) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    sched_mfma_two_lds_reads<N - 1>();
+  }
+}
 // The step's R LDS reads and then its D LDS-DMA loads, each behind one of the step's first MFMAs.  The loads come last, as in
 // the source: they write LDS, so the compiler moves no LDS read across them, and groups that ask for a load between two
 // reads are not followed at all (the reads then run in one burst; 16384 tokens x 4096 x 11008: gate/up 4.66 -> 4.50 ms,
@@ -113,7 +122,7 @@ struct GemmArgs {
 struct DenseArgs : GemmArgs {  // K: elements of a slice
   int M, MT;             // rows, row tiles
   int slices;
-  int lda, ldb;          // elements between rows of A and of B (turned operands: of their memory); gemm_tile_kernel: the same
+  int lda, ldb;          // elements between rows of A and of B (turned operands: of their memory)
   int Kall;              // elements of the whole summation
   const float *bias;     // [R], R = N, gated 2 N (B1 = B0 + N rows); or NULL
   const void *residual;  // [M, N] or NULL
@@ -290,24 +299,39 @@ constexpr int PK_SMEM = PK_B_BASE + PK_B_STAGES * PK_B_STAGE;  // 160 KB: all of
 [[maybe_unused]] constexpr int PK_NI = (PK_BM + PK_BROWS) / 8 / PK_NW;  // 1 KB load instructions per wave per chunk
 [[maybe_unused]] constexpr int PK_NIA = PK_BM / 8 / PK_NW;
 
-// Turned operands (TA, TB; dense products): the summation runs down the memory's rows, as in dx = dz W and dw = dz^T x.  A chunk
-// is then 64 memory rows of 256 neighbouring columns, 512 bytes each, staged as they lie (a DMA instruction fills two), and the
-// fragments come out of LDS through ds_read_b64_tr_b16: 16 lanes name the 4 pieces of 8 bytes of each of 4 rows, and lane l gets
-// column l of the four.  A lane's eight elements are two such reads, rows 8 g .. + 3 and + 4 .. + 7 (g = lane / 16), as in an
-// operand that is not turned.  32-byte unit c of row k sits at c ^ turn_swz(k): the eight rows that 32 lanes read at once
-// then lie in different eighths of the 64 banks.  Rows past the end of the summation read as zero (range check), columns past the
-// operand's edge hold the next row's and are not stored.
-__device__ inline int turn_swz(int k) { return (k & 3) | (k >> 1 & 4); }
-constexpr int TR_ROW_BYTES = 512;
+// Turned operands (TA, TB; dense products, bf16): the summation runs down the memory's rows, as in dx = dz W and dw = dz^T x.  A
+// chunk is then 64 memory rows of as many neighbouring columns as the tile has rows, staged as they lie (a DMA instruction fills
+// 1 KB of them), and the fragments come out of LDS through ds_read_b64_tr_b16: 16 lanes name the 4 pieces of 8 bytes of each of
+// 4 rows, and lane l gets column l of the four.  A lane's eight elements are two such reads, rows 8 g .. + 3 and + 4 .. + 7
+// (g = lane / 16), as in an operand that is not turned.  32-byte unit c of staged row k sits at c ^ turn_swz(k): the eight rows that
+// 32 lanes read at once then lie in different eighths of the 64 banks, whatever the row's length RB (64 to 512 bytes; four or two short
+// rows share the banks).  Rows past the end of the summation read as zero (range check), columns past the operand's edge hold
+// the next row's and are not stored.
+template <int RB>
+__device__ inline int turn_swz(int k) {
+  return RB >= 256 ? (k & 3) | (k >> 1 & 4) : RB == 128 ? (k >> 1 & 1) | (k >> 2 & 2) : k >> 3 & 1;
+}
 typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
+// This lane's place in a DMA instruction that fills staged rows from `first` on: its row, and the byte of the memory row it fetches.
+template <int RB>
+__device__ inline void turned_lane(int first, int lane, int &row, int &byte) {
+  row = first + lane / (RB / 16);
+  byte = ((lane % (RB / 16)) ^ turn_swz<RB>(row) << 1) * 16;
+}
+// This lane's first row of a 32 x 16 fragment of unit c.
+template <int RB>
+__device__ inline int turned_at(int c, int fr, int fg) {
+  const int k = 8 * fg + (fr >> 2);
+  return k * RB + (c ^ turn_swz<RB>(k)) * 32 + (fr & 3) * 8;
+}
 // A turned fragment of 32 x 16 elements whose first row of this lane is at `at` in LDS.  (__restrict__ is not about aliases here: it
 // leaves a scope on the reads, without which the compiler takes them for possible readers of every DMA load under way and drains
 // those, vmcnt(0), before each group of reads.)
+template <int RB>
 __device__ __forceinline__ bf16x8 read_turned(const char *__restrict__ at) {
 #if defined(__HIP_DEVICE_COMPILE__)
   const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)at);
-  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(at + 4 * TR_ROW_BYTES));
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)(at + 4 * RB));
   return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #else
   return bf16x8{};
@@ -381,12 +405,13 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
   const int b_off = (wn * (GATED ? WN / 2 : WN) * 16 + fr) * GB_ROW_BYTES;
   // turned operands: the lane's offset for fragment i (A: i % 4; the others are 256 bytes further), first row
   int a_turn[4], b_turn[WN];
+  constexpr int TRB = PK_BM * 2;  // bytes of a staged row
+  static_assert(PK_BROWS == PK_BM);
   if constexpr (TA || TB) {
-    const int k = 8 * fg + (fr >> 2), f = turn_swz(k), at = k * TR_ROW_BYTES + (fr & 3) * 8;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a_turn[i] = at + ((i * PK_WAVES_M + wm) ^ f) * 32;
+    for (int i = 0; i < 4; ++i) a_turn[i] = turned_at<TRB>(i * PK_WAVES_M + wm, fr, fg);
 #pragma unroll
-    for (int j = 0; j < WN; ++j) b_turn[j] = at + ((wn * WN + j) ^ f) * 32;
+    for (int j = 0; j < WN; ++j) b_turn[j] = turned_at<TRB>(wn * WN + j, fr, fg);
   }
   auto b_frag = [&](int j) { return (GATED && j >= WN / 2 ? BN + (j - WN / 2) * 16 : j * 16) * GB_ROW_BYTES; };
 
@@ -427,7 +452,8 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
   }
   // bytes between the rows of consecutive instructions
   const unsigned rstep = NW * (TA ? 2 : 8) * lda * 2, rstep_b = NW * (TB ? 2 : 8) * ldb * 2;
-  const int trow = w * 2 + (lane >> 5), tcol = ((lane & 31) ^ turn_swz(trow) << 1) * 16;  // turned: as lrow and lcol
+  int trow = 0, tcol = 0;  // turned: as lrow and lcol
+  if constexpr (TA || TB) turned_lane<TRB>(w * 2, lane, trow, tcol);
   static_assert(NW * 2 % 16 == 0, "the swizzle of a turned operand must not depend on the instruction index");
   // this lane's piece of the last chunk lies past the end of the row (K no multiple of the chunk)
   const bool past = (KT - 1) * GB_BK * 2 + lcol >= K * 2;
@@ -651,7 +677,7 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
 #pragma unroll
         for (int i = 0; i < HM; ++i)
           if constexpr (TA)
-            af[hf][i] = read_turned(sta + a_turn[(hf * HM + i) & 3] + (hf * HM + i) / 4 * 256 + ks * 32 * TR_ROW_BYTES);
+            af[hf][i] = read_turned<TRB>(sta + a_turn[(hf * HM + i) & 3] + (hf * HM + i) / 4 * 256 + ks * 32 * TRB);
           else
             af[hf][i] = *reinterpret_cast<const bf16x8 *>(p + (hf * HM + i) * PK_WAVES_M * 16 * GB_ROW_BYTES);
       };
@@ -659,7 +685,7 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
         const char *p = stb + b_off + (((4 * ks + fg) ^ fsw) << 4);
 #pragma unroll
         for (int j = 0; j < WN; ++j)
-          if constexpr (TB) bfr[ks][j] = read_turned(stb + b_turn[j] + ks * 32 * TR_ROW_BYTES);
+          if constexpr (TB) bfr[ks][j] = read_turned<TRB>(stb + b_turn[j] + ks * 32 * TRB);
           else bfr[ks][j] = *reinterpret_cast<const bf16x8 *>(p + b_frag(j));
       };
       auto mfma_step = [&](int ks, int hf) {
@@ -842,7 +868,7 @@ struct TileShape {
 };
 
 // ACT: RR_ACT_GELU, RR_ACT_SWIGLU (bf16: with the division), or -1
-template <class S, bool GATED, int ACT, bool GATHER, bool DIRECT, bool DENSE = false>
+template <class S, bool GATED, int ACT, bool GATHER, bool DIRECT, bool DENSE = false, bool TA = false, bool TB = false>
 __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename std::conditional<DENSE, DenseArgs, GemmArgs>::type P) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int WM = S::WM, WN = S::WN, NW = S::NW, BM = S::BM, ST = S::ST;
@@ -852,6 +878,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "operand boundaries must fall between load instructions");
   static_assert((8 * NW) % 16 == 0, "swizzle must not depend on the instruction index");
   static_assert(!GATED || WN % 2 == 0, "a wave holds the gate and the up columns of its outputs");
+  static_assert(!(TA || TB) || (DENSE && !GATED && !GATHER && S::BF16));
   constexpr int kPanel = 8;  // row tiles that share a column tile of weights before the next column tile
   extern __shared__ __attribute__((aligned(16))) char smem[];
 
@@ -868,7 +895,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   const int panel = t / (kPanel * NT), r = t - panel * kPanel * NT, h = min(kPanel, MT - panel * kPanel);
   const int nt = r / h, mt = panel * kPanel + r - nt * h;
   TileInfo ti;
-  int m0, K = P.K, LD = K, k0 = 0;
+  int m0, K = P.K, LD = K, LDB = K, k0 = 0;
   if constexpr (DENSE) {
     const int slice = mt / P.MT;
     ti = TileInfo{slice, 0, 0, P.M, 0, 0, 0, 0};
@@ -876,6 +903,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     k0 = slice * K;
     K = min(K, P.Kall - k0);
     LD = P.lda;
+    LDB = P.ldb;
   } else {
     ti = P.tiles[mt / P.sub];
     m0 = ti.row0 + mt % P.sub * BM;
@@ -893,13 +921,14 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   const int lrow = w * 8 + (lane >> 3);            // stage row of this lane in instruction 0
   const int piece = S::MATH == TILE_SPLIT ? lane & 7 : (lane & 7) ^ swz(lrow);  // 16-byte piece of the row's chunk that belongs at its position
   const unsigned rowb = (unsigned)LD * ES;
-  const unsigned rstep = NW * 8 * rowb;            // between the rows of consecutive instructions
+  const unsigned rowbB = DENSE ? (unsigned)LDB * ES : rowb;
+  const unsigned rstep = NW * 8 * rowb, rstepB = DENSE ? NW * 8 * rowbB : rstep;  // between the rows of consecutive instructions
   auto rsrc = [](const char *base, size_t off, long long range) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base) + off, 0,
                                              __builtin_amdgcn_readfirstlane((int)range), BUF_FLAGS);
   };
-  const size_t mat = (DENSE ? (size_t)k0 * ES : (size_t)e * N * K * ES) + (size_t)n0 * rowb;
-  const long long brange = (long long)min(BN, N - n0) * rowb - k0 * ES;
+  const size_t mat = (DENSE ? (size_t)k0 * ES : (size_t)e * N * K * ES) + (size_t)n0 * rowbB;
+  const long long brange = (long long)min(BN, N - n0) * rowbB - k0 * ES;
   const __amdgpu_buffer_rsrc_t rsB0 = rsrc(static_cast<const char *>(P.B0), mat, brange);
   const __amdgpu_buffer_rsrc_t rsB1 = GATED ? rsrc(static_cast<const char *>(P.B1), mat, brange) : rsB0;
   const __amdgpu_buffer_rsrc_t rsA =
@@ -923,20 +952,50 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   } else {
     va[0] = lrow * rowb + piece * 16;
   }
-  const unsigned vb = lrow * rowb + piece * 16;
+  const unsigned vb = lrow * rowbB + piece * 16;
+  // Turned operands: a chunk's rows are a buffer of their own, from the tile's first column on.  Offsets of this lane in instructions
+  // 0 and 1 (the swizzle of two instructions apart is the same), bytes between instructions.
+  constexpr int TRA = BM * 2, TRB = S::BROWS * 2, RPA = 1024 / TRA, RPB = 1024 / TRB;
+  static_assert(!TA || NW * RPA % 8 == 0);
+  static_assert(!TB || NW * RPB % 8 == 0);
+  unsigned ta[2] = {0, 0}, tb[2] = {0, 0};
+  if constexpr (TA || TB) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int row, byte;
+      turned_lane<TRA>((i * NW + w) * RPA, lane, row, byte);
+      ta[i] = (row - i * NW * RPA) * rowb + byte;
+      turned_lane<TRB>((i * NW + w) * RPB, lane, row, byte);
+      tb[i] = (row - i * NW * RPB) * rowbB + byte;
+    }
+  }
+  auto turned_rsrc = [&](const void *base, int kt, unsigned pitch, int col) {
+    const int rows = kt < KT ? min(CE, K - kt * CE) : 0;  // past the end: none
+    return rsrc(static_cast<const char *>(base), (size_t)(k0 + min(kt, KT - 1) * CE) * pitch + col * ES,
+                rows > 0 ? (long long)rows * pitch - col * ES : 0);
+  };
   auto issue = [&](int kt, int stage) {
     char *st = smem + stage * S::STAGE + w * 1024;
     const bool past = kt * CE + piece * PE >= K;  // the last chunk of a ragged K, and chunks past the end
     const int koff = min(kt, KT - 1) * GB_ROW_BYTES;
+    const __amdgpu_buffer_rsrc_t rsTB = TB ? turned_rsrc(P.B0, kt, rowbB, n0) : rsB0, rsTA = TA ? turned_rsrc(P.A, kt, rowb, m0) : rsA;
 #pragma unroll
     for (int i = 0; i < NIB; ++i) {
       auto lp = (__attribute__((address_space(3))) void *)(st + BM * GB_ROW_BYTES + i * NW * 1024);
-      const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstep;
+      if constexpr (TB) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsTB, lp, 16, tb[i & 1] + i * NW * RPB * rowbB, 0, 0, 0);
+        continue;
+      }
+      const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstepB;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(!GATED || i < NIB0 ? rsB0 : rsB1, lp, 16, past ? PAST : v, koff, 0, 0);
     }
 #pragma unroll
     for (int i = 0; i < NIA; ++i) {
       auto lp = (__attribute__((address_space(3))) void *)(st + i * NW * 1024);
+      if constexpr (TA) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsTA, lp, 16, ta[i & 1] + i * NW * RPA * rowb, 0, 0, 0);
+        continue;
+      }
       const unsigned v = GATHER ? va[GATHER ? i : 0] : va[0] + i * rstep;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rsA, lp, 16, past ? PAST : v, koff, 0, 0);
     }
@@ -954,6 +1013,13 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     if (GATED) row = (j < H) ? (wn * H + j) * 16 + fr : BN + (wn * H + (j - H)) * 16 + fr;
     b_off[j] = (BM + row) * GB_ROW_BYTES;
   }
+  int a_turn[WM], b_turn[WN];
+  if constexpr (TA || TB) {
+#pragma unroll
+    for (int i = 0; i < WM; ++i) a_turn[i] = turned_at<TRA>(wm * WM + i, fr, fg);
+#pragma unroll
+    for (int j = 0; j < WN; ++j) b_turn[j] = BM * GB_ROW_BYTES + turned_at<TRB>(wn * WN + j, fr, fg);
+  }
   using Frag = typename std::conditional<S::BF16, bf16x8, f32x4>::type;
   f32x4 acc[WM][WN];
 #pragma unroll
@@ -964,9 +1030,15 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   auto load_frags = [&](const char *st, int ks) {
     const int pos = ((4 * ks + fg) ^ fsw) << 4;
 #pragma unroll
-    for (int i = 0; i < WM; ++i) af[ks][i] = *reinterpret_cast<const Frag *>(st + a_off[i] + pos);
+    for (int i = 0; i < WM; ++i) {
+      if constexpr (TA) af[ks][i] = read_turned<TRA>(st + a_turn[i] + ks * 32 * TRA);
+      else af[ks][i] = *reinterpret_cast<const Frag *>(st + a_off[i] + pos);
+    }
 #pragma unroll
-    for (int j = 0; j < WN; ++j) bfr[ks][j] = *reinterpret_cast<const Frag *>(st + b_off[j] + pos);
+    for (int j = 0; j < WN; ++j) {
+      if constexpr (TB) bfr[ks][j] = read_turned<TRB>(st + b_turn[j] + ks * 32 * TRB);
+      else bfr[ks][j] = *reinterpret_cast<const Frag *>(st + b_off[j] + pos);
+    }
   };
   // B fragment first: the accumulator holds the transposed tile, a lane owns row (lane & 15) of the A
   // fragment and four consecutive columns, 4 * (lane >> 4) .. + 3 of the B fragment
@@ -1007,7 +1079,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
       const int koff = min(kt, KT - 1) * GB_ROW_BYTES;
 #pragma unroll
       for (int i = 0; i < NIB; ++i) {
-        const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstep;
+        const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstepB;
         raw[NIA + i] = load16(!GATED || i < NIB0 ? rsB0 : rsB1, past ? PAST : v, koff);
       }
 #pragma unroll
@@ -1100,7 +1172,8 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
       __builtin_amdgcn_sched_barrier(0);
       load_frags(st, 1);
       mfma_step(0);
-      if constexpr (S::BF16) sched_mfma_lds_read<(WM + WN < WM * WN ? WM + WN : WM * WN)>();
+      if constexpr (TA || TB) sched_mfma_two_lds_reads<(WM + WN < WM * WN ? WM + WN : WM * WN)>();
+      else if constexpr (S::BF16) sched_mfma_lds_read<(WM + WN < WM * WN ? WM + WN : WM * WN)>();
       __builtin_amdgcn_sched_barrier(0);
       cur = cur == ST - 1 ? 0 : cur + 1;
       fill = fill == ST - 1 ? 0 : fill + 1;

@@ -2,8 +2,8 @@
 //
 // Every product is "A[rows, K] times B[N, K]^T" with K contiguous in both operands (rr_gemm.h):
 //   forward  x, W                 dx  dz, W^T                 dw  dz^T, x^T
-// The 256 x 256 tiles read the operands of the gradients as they lie in memory ("turned" operands); for the other tiles
-// linear_turn_kernel writes the transposes.  It also makes dz from dy and the stored z, and sums its columns.
+// bf16 tiles read the operands of the gradients as they lie in memory ("turned" operands); for fp32 ones linear_turn_kernel
+// writes the transposes.  It also makes dz from dy and the stored z, and sums its columns.
 // Which kernel multiplies is a matter of estimated time (dense_plan): 256 x 256 tiles of the persistent kernel, smaller
 // tiles, either with the summation cut into slices where the tiles alone would leave CUs idle (each slice's raw sums go
 // to the workspace and linear_join_kernel adds them in order and does the epilogue), or, up to kFewRows rows,
@@ -366,9 +366,9 @@ size_t part_reserve(size_t M, size_t R) { return up256(std::min(part_bytes(M, R,
 
 struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_kernel
 
-// Times in us of a dense product's parts: a fit to 750 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 300 fp32
-// ones, each timed in up to 26 pairs of shape and slices.  The plan is 1.3 % (fp32: 2.2 %) off the best pair on average, 1.8 %
-// (3.0 %) on the quarter of them that the fit did not see; the worst of those by 27 % (25 %), of products of 4 us.  (The grouped GEMM's
+// Times in us of a dense product's parts: a fit to 750 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 550 fp32
+// ones, each timed in up to 26 pairs of shape and slices.  The plan is 1.3 % (fp32: 2.3 %) off the best pair on average, 1.8 %
+// (2.8 %) on the quarter of them that the fit did not see; the worst of those by 27 % (25 %), of products of 4 us.  (The grouped GEMM's
 // numbers, which expect ragged experts and weights from HBM: 7 %, the worst by 45 %.)
 struct DenseShape { float chunk, fixed, alone; };  // as ShapeInfo: of a chunk, of a tile, of a chunk with the CU to itself (split shapes)
 struct DenseTimes {
@@ -377,18 +377,17 @@ struct DenseTimes {
   float fetch, stream;   // bytes per us that a CU gets of its operands, and all of them together
   float last, even;      // a last, partial round on top of its share; split shapes: weight of the exact number of rounds
   float launch, join, join_slice, join_bytes;  // of any kernel; of the joining one: itself, per slice, passes over the slices' sums
+  float rows;            // linear_rows_kernel: start and end
 };
 constexpr DenseTimes kBf16Times{FFN_P256, {{1.345f, 0.02f}, {0.80f, 0.68f}, {0.474f, 1.07f}, {0.379f, 0.04f}, {0.267f, 0.93f}, {0.129f, 1.29f}},
-                                122e3f, 10.1e6f, 0.88f, 0.0f, 2.5f, 1.7f, 0.19f, 2.1f};
-constexpr DenseTimes kF32Times{FFN_S128, {{1.334f, 0.86f, 1.81f}, {0.734f, 0.51f, 0.81f}, {0.859f, 1.09f}, {0.501f, 0.35f}, {0.251f, 0.16f}, {0.0f, 0.0f}},
-                               57.7e3f, 4.66e6f, 0.61f, 0.27f, 3.7f, 2.2f, 0.12f, 0.91f};
+                                122e3f, 10.1e6f, 0.88f, 0.0f, 2.5f, 1.7f, 0.19f, 2.1f, 1.1f};
+constexpr DenseTimes kF32Times{FFN_S128, {{1.328f, 1.38f, 1.61f}, {0.74f, 0.63f, 0.87f}, {0.914f, 0.50f}, {0.515f, 0.29f}, {0.26f, 0.03f}, {0.0f, 0.0f}},
+                               45.5e3f, 130e6f, 0.66f, 0.19f, 3.4f, 2.1f, 0.14f, 0.90f, 0.1f};
 constexpr float kPersistentDense = 2.9f;  // the 256 x 256 kernel's start
 constexpr float kTurnedBoth = 1.15f;      // its K loop with both operands turned: twice the LDS reads
-constexpr float kTurnLaunch = 3.0f, kTurnBytes = 4.5e6f;
 
 // Estimated time of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
-// turned: the operands lie the other way round.  Only the 256 x 256 tiles read those as they are; for the others the time of
-// writing transposes is counted.
+// turned: B, or both operands, lie the other way round (fp32: after the transposes, which every plan needs, they do not).
 enum Turned { TURNED_NONE, TURNED_B, TURNED_BOTH };
 float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, Turned turned, int q, int slices) {
   constexpr int kCUs = 256;
@@ -407,7 +406,7 @@ float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, T
   if (slices > 1 && part > kPartBytes) return -1.0f;
   const float stream = (float)((double)(M + R) * K * es + (double)M * N * es) / T.stream;
   const float fetch = (float)GB_ROW_BYTES * ((float)s.brows / mt + (float)s.bm / nt) / T.fetch;
-  const float chunk = std::max(c.chunk * (turned == TURNED_BOTH && persistent ? kTurnedBoth : 1.0f), fetch);
+  const float chunk = std::max(c.chunk * (turned == TURNED_BOTH && bf16 ? kTurnedBoth : 1.0f), fetch);
   float busy = (float)rounds * (KT * chunk + c.fixed);
   if (split) {
     const float all = (float)tiles / kCUs;
@@ -420,30 +419,27 @@ float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, T
   }
   float t = T.launch + std::max(busy, stream) + 0.1f * busy;
   if (slices > 1) t += T.join + T.join_slice * slices + T.join_bytes * (float)part / kHbm;
-  if (turned != TURNED_NONE && !persistent)
-    t += kTurnLaunch + (float)((2 * N * K + (turned == TURNED_BOTH ? M * K : 0)) * es) / kTurnBytes;
   return t;
 }
 
 // linear_rows_kernel: a workgroup reads its rows of W and all of A.
-float rows_cost(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
+float rows_cost(long long M, long long N, long long K, bool bf16, bool gated) {
   const DenseTimes &T = bf16 ? kBf16Times : kF32Times;
   const int es = bf16 ? 2 : 4;
   const long long blocks = (N + 15) / 16, bytes = ((gated ? 32 : 16) + M) * K * es;
-  constexpr float kAlone = 42.5e3f, kShared = 30.5e3f;  // bytes per us of a CU with one workgroup, with several
-  float t = T.launch + 1.1f + (float)((blocks + 255) / 256) * (float)bytes / (blocks > 256 ? kShared : kAlone);
-  if (turned != TURNED_NONE) t += kTurnLaunch + (float)((2 * N * K + (turned == TURNED_BOTH ? M * K : 0)) * es) / kTurnBytes;
-  return t;
+  constexpr float kAlone = 42e3f, kShared = 30e3f;  // bytes per us of a CU with one workgroup, with several
+  return T.launch + T.rows + (float)((blocks + 255) / 256) * (float)bytes / (blocks > 256 ? kShared : kAlone);
 }
 
 DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
-  if (M <= kVectorRows) return {-1, 1};
+  const bool as_is = bf16 && turned != TURNED_NONE;  // tiles only
+  if (M <= kVectorRows && !as_is) return {-1, 1};
   const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : FFN_F32N;
   DensePlan best{q1, 1};
   float least = -1.0f;
-  if (M <= kFewRows) {
+  if (M <= kFewRows && !as_is) {
     best = {-1, 1};
-    least = rows_cost(M, N, K, bf16, gated, turned);
+    least = rows_cost(M, N, K, bf16, gated);
   }
   for (int q = q0; q <= q1; ++q) {
     const long long bn = gated ? kShape[q].brows / 2 : kShape[q].brows, tiles = (M + kShape[q].bm - 1) / kShape[q].bm * ((N + bn - 1) / bn);
@@ -455,7 +451,7 @@ DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gate
   return best;
 }
 
-template <class S, bool GATED, int ACT>
+template <class S, bool GATED, int ACT, bool TA, bool TB>
 void launch_dense_tiles(DenseArgs A, hipStream_t s) {
   constexpr int bn = GATED ? S::BROWS / 2 : S::BROWS;
   A.NT = (A.N + bn - 1) / bn;
@@ -463,38 +459,36 @@ void launch_dense_tiles(DenseArgs A, hipStream_t s) {
   constexpr long long kRow = 1ll << 20;  // workgroups in a row of the grid, whole XCD runs (see gemm_tile_kernel)
   const long long tiles = (long long)A.NT * A.MT * A.slices;
   const dim3 grid((unsigned)((std::min(tiles, kRow) + 7) / 8 * 8), (unsigned)((tiles + kRow - 1) / kRow));
-  gemm_tile_kernel<S, GATED, ACT, false, false, true><<<grid, S::THREADS, S::SMEM, s>>>(A);
+  gemm_tile_kernel<S, GATED, ACT, false, false, true, TA, TB><<<grid, S::THREADS, S::SMEM, s>>>(A);
 }
 
-template <bool BF16, bool GATED, int ACT>
-void launch_dense_shape(int shape, const DenseArgs &A0, hipStream_t s) {
-  DenseArgs A = A0;
+template <bool BF16, bool GATED, int ACT, bool TA = false, bool TB = false>
+void launch_dense_shape(int shape, DenseArgs A, hipStream_t s) {
   if constexpr (BF16) {
     switch (shape) {
       case FFN_P256:
         A.NT = GATED ? (A.N + 127) / 128 : (A.N + 255) / 256;
         A.MT = (A.M + PK_BM - 1) / PK_BM;
-        gemm_bf16_persistent_kernel<GATED, ACT, false, false, true><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
+        gemm_bf16_persistent_kernel<GATED, ACT, false, false, true, TA, TB><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
         break;
-      case FFN_256: launch_dense_tiles<TileB256, GATED, ACT>(A, s); break;
-      case FFN_128: launch_dense_tiles<TileB128, GATED, ACT>(A, s); break;
-      case FFN_64: launch_dense_tiles<TileB64, GATED, ACT>(A, s); break;
-      case FFN_32: launch_dense_tiles<TileB32, GATED, ACT>(A, s); break;
-      default: launch_dense_tiles<TileB32n, GATED, ACT>(A, s); break;
+      case FFN_256: launch_dense_tiles<TileB256, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_128: launch_dense_tiles<TileB128, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_64: launch_dense_tiles<TileB64, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_32: launch_dense_tiles<TileB32, GATED, ACT, TA, TB>(A, s); break;
+      default: launch_dense_tiles<TileB32n, GATED, ACT, TA, TB>(A, s); break;
     }
   } else {
     switch (shape) {
-      case FFN_S128: launch_dense_tiles<TileS128, GATED, ACT>(A, s); break;
-      case FFN_S64: launch_dense_tiles<TileS64, GATED, ACT>(A, s); break;
-      case FFN_F64: launch_dense_tiles<TileF64, GATED, ACT>(A, s); break;
-      case FFN_F32: launch_dense_tiles<TileF32, GATED, ACT>(A, s); break;
-      default: launch_dense_tiles<TileF32n, GATED, ACT>(A, s); break;
+      case FFN_S128: launch_dense_tiles<TileS128, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_S64: launch_dense_tiles<TileS64, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_F64: launch_dense_tiles<TileF64, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_F32: launch_dense_tiles<TileF32, GATED, ACT, TA, TB>(A, s); break;
+      default: launch_dense_tiles<TileF32n, GATED, ACT, TA, TB>(A, s); break;
     }
   }
 }
 
-// The product and its epilogue.  A.A, B0, B1, Cout, M, N, lda, ldb, Kall and the epilogue's pointers are set.  turned: only with
-// a plan of 256 x 256 tiles.
+// The product and its epilogue.  A.A, B0, B1, Cout, M, N, lda, ldb, Kall and the epilogue's pointers are set.
 template <bool BF16, bool GATED, int ACT>
 void launch_product(DenseArgs A, const DensePlan &plan, Turned turned, float *part, hipStream_t s) {
   constexpr int ce = GB_ROW_BYTES / (BF16 ? 2 : 4);
@@ -517,14 +511,11 @@ void launch_product(DenseArgs A, const DensePlan &plan, Turned turned, float *pa
     else linear_rows_kernel<BF16, GATED, ACT, 2><<<grid, LR_THREADS, 0, s>>>(A);
     return;
   }
-  if (turned == TURNED_NONE) {
-    launch_dense_shape<BF16, GATED, ACT>(plan.shape, A, s);
-  } else if constexpr (BF16 && !GATED && ACT < 0) {
-    A.NT = (A.N + PK_BROWS - 1) / PK_BROWS;
-    A.MT = (A.M + PK_BM - 1) / PK_BM;
-    if (turned == TURNED_B) gemm_bf16_persistent_kernel<false, -1, false, false, true, false, true><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
-    else gemm_bf16_persistent_kernel<false, -1, false, false, true, true, true><<<cu_count(), PK_THREADS, PK_SMEM, s>>>(A);
+  if constexpr (BF16 && !GATED && ACT < 0) {
+    if (turned == TURNED_B) launch_dense_shape<BF16, GATED, ACT, false, true>(plan.shape, A, s);
+    if (turned == TURNED_BOTH) launch_dense_shape<BF16, GATED, ACT, true, true>(plan.shape, A, s);
   }
+  if (turned == TURNED_NONE) launch_dense_shape<BF16, GATED, ACT>(plan.shape, A, s);
   if (plan.slices > 1)
     linear_join_kernel<BF16, GATED, ACT><<<(unsigned)(((size_t)A.M * (A.N / 4) + 255) / 256), 256, 0, s>>>(A);
 }
@@ -565,9 +556,10 @@ BackwardWork backward_work(const rr_linear_config &c, void *ws) {
   const size_t R = width(c), es = element(c);
   W.LT = (c.M + 63) / 64 * 64;
   W.dz = take(c.act == RR_ACT_NONE ? 0 : (size_t)c.M * R * es);
-  W.dz_turned = take(R * W.LT * es);
-  W.x_turned = take((size_t)c.K * W.LT * es);
-  W.w_turned = take((size_t)c.K * R * es);
+  const bool turns = c.dtype != RR_BF16;
+  W.dz_turned = take(turns ? R * W.LT * es : 0);
+  W.x_turned = take(turns ? (size_t)c.K * W.LT * es : 0);
+  W.w_turned = take(turns ? (size_t)c.K * R * es : 0);
   W.sums = static_cast<float *>(take((size_t)(W.LT / TN_TILE) * R * 4));
   W.part = static_cast<float *>(take(std::max(part_reserve(c.M, c.K), part_reserve(R, c.K))));
   W.bytes = off;
@@ -586,6 +578,10 @@ hipError_t linear_kernel_attributes() {
     set(gemm_tile_kernel<S, true, -1, false, false, true>, S::SMEM);
     set(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false, true>, S::SMEM);
     set(gemm_tile_kernel<S, false, -1, false, false, true>, S::SMEM);
+    if constexpr (S::BF16) {
+      set(gemm_tile_kernel<S, false, -1, false, false, true, false, true>, S::SMEM);
+      set(gemm_tile_kernel<S, false, -1, false, false, true, true, true>, S::SMEM);
+    }
   };
   for_each_tile_shape(kinds);
   set(gemm_bf16_persistent_kernel<true, -1, false, false, true>, PK_SMEM);
@@ -656,21 +652,20 @@ hipError_t launch_linear_backward(const rr_linear_config &c, const void *x, cons
   };
   const bool act = c.act != RR_ACT_NONE;
   const DensePlan plan_x = dense_plan(c.M, c.K, R, bf16, false, TURNED_B), plan_w = dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH);
-  const bool as_is_x = plan_x.shape == FFN_P256, as_is_w = plan_w.shape == FFN_P256;  // no transposes
-  const TurnArgs make{dy, pre, act && (dx || (dw && as_is_w)) ? W.dz : nullptr, dw && !as_is_w ? W.dz_turned : nullptr,
+  const TurnArgs make{dy, pre, act && (dx || (dw && bf16)) ? W.dz : nullptr, dw && !bf16 ? W.dz_turned : nullptr,
                       dbias ? W.sums : nullptr, c.M, c.N, W.LT};
   const void *dz = act ? W.dz : dy;
   prof_begin(K_LINEAR_BWD, s);
   if (make.dz || make.turned || make.sums) turn(c.act, make);
   if (dbias) linear_bias_kernel<<<(R + kWave - 1) / kWave, 256, 0, s>>>(W.sums, (c.M + TN_TILE - 1) / TN_TILE, R, dbias);
   if (dx) {
-    if (!as_is_x) turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
-    if (as_is_x) product(dz, R, w, c.K, dx, c.M, c.K, R, plan_x, TURNED_B);
+    if (!bf16) turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
+    if (bf16) product(dz, R, w, c.K, dx, c.M, c.K, R, plan_x, TURNED_B);
     else product(dz, R, W.w_turned, R, dx, c.M, c.K, R, plan_x, TURNED_NONE);
   }
   if (dw) {
-    if (!as_is_w) turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
-    if (as_is_w) product(dz, R, x, c.K, dw, R, c.K, c.M, plan_w, TURNED_BOTH);
+    if (!bf16) turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
+    if (bf16) product(dz, R, x, c.K, dw, R, c.K, c.M, plan_w, TURNED_BOTH);
     else product(W.dz_turned, W.LT, W.x_turned, W.LT, dw, R, c.K, W.LT, plan_w, TURNED_NONE);
   }
   prof_end(K_LINEAR_BWD, s);
