@@ -78,14 +78,6 @@ __device__ inline float row_sum(float v) {
   if (LANES >= 16) v += dpp<0x140>(v);
   return v;
 }
-// exp(x) for x <= 0 to 2 u: 2^t with t the rounded x / ln 2, times 1 + ln 2 (x / ln 2 - t); 0 where it is below 2^-126, and for
-// -infinity.  (Half of expf's instructions, which bind the loss.)
-__device__ inline float exp_short(float x) {
-  constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = (float)(1.44269504088896341 - (double)kLog2e), kLn2 = 0.69314718055994531f;
-  x = x < -104.0f ? -104.0f : x;  // (NaN stays)
-  const float t = x * kLog2e, r = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
-  return fmaf(e * r, kLn2, e);
-}
 // Scores -> unnormalised probabilities; returns 1 / their sum (0 for a row of -infinity only).
 template <int LANES>
 __device__ inline float softmax_row(float (&a)[4]) {

@@ -113,4 +113,13 @@ __device__ inline u32 pack_bf16(float a, float b) {
 // 5 times the error for |g| < 1: 41 of 2^20 normal arguments of sigma 0.3 round to another bf16 than g Phi(g) does, here 3.)
 __device__ inline float gelu_erf(float g) { return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f)); }
 
+// exp(x) for x <= 0 to 2 u: 2^t with t the rounded x / ln 2, times 1 + ln 2 (x / ln 2 - t); 0 where it is below 2^-126, and for
+// -infinity.  (Half of expf's instructions, which bind the loss.)
+__device__ inline float exp_short(float x) {
+  constexpr float kLog2e = 1.44269504088896341f, kLog2eLow = (float)(1.44269504088896341 - (double)kLog2e), kLn2 = 0.69314718055994531f;
+  x = x < -104.0f ? -104.0f : x;  // (NaN stays)
+  const float t = x * kLog2e, r = fmaf(x, kLog2eLow, fmaf(x, kLog2e, -t)), e = __builtin_amdgcn_exp2f(t);
+  return fmaf(e * r, kLn2, e);
+}
+
 }  // namespace rr
