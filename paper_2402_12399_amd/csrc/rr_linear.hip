@@ -422,10 +422,10 @@ size_t part_reserve(size_t M, size_t R) { return up256(std::min(part_bytes(M, R,
 
 struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_kernel
 
-// Times in us of a dense product's parts: a fit to 750 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 550 fp32
-// ones, each timed in up to 26 pairs of shape and slices.  The plan is 1.3 % (fp32: 2.3 %) off the best pair on average, 1.8 %
-// (2.8 %) on the quarter of them that the fit did not see; the worst of those by 27 % (25 %), of products of 4 us.  (The grouped GEMM's
-// numbers, which expect ragged experts and weights from HBM: 7 %, the worst by 45 %.)
+// Times in us of a dense product's parts: a fit to 970 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 700 fp32
+// ones, each timed in up to 34 pairs of shape and slices.  The plan is 1.2 % (fp32: 1.1 %) off the best pair on average, 1.4 %
+// (1.4 %) on the quarter of them that the fit did not see; the worst of those by 24 % (21 %), most of them products of 4 us.  (The
+// grouped GEMM's numbers, which expect ragged experts and weights from HBM: 7 %, the worst by 45 %.)
 struct DenseShape { float chunk, fixed, alone; };  // as ShapeInfo: of a chunk, of a tile, of a chunk with the CU to itself (split shapes)
 struct DenseTimes {
   int first;             // FfnShape of shape[0]
@@ -435,12 +435,11 @@ struct DenseTimes {
   float launch, join, join_slice, join_bytes;  // of any kernel; of the joining one: itself, per slice, passes over the slices' sums
   float rows;            // linear_rows_kernel: start and end
 };
-constexpr DenseTimes kBf16Times{FFN_P256, {{1.345f, 0.02f}, {0.80f, 0.68f}, {0.474f, 1.07f}, {0.379f, 0.04f}, {0.267f, 0.93f}, {0.129f, 1.29f}},
-                                122e3f, 10.1e6f, 0.88f, 0.0f, 2.5f, 1.7f, 0.19f, 2.1f, 1.1f};
-constexpr DenseTimes kF32Times{FFN_S128, {{1.328f, 1.38f, 1.61f}, {0.74f, 0.63f, 0.87f}, {0.914f, 0.50f}, {0.515f, 0.29f}, {0.26f, 0.03f}, {0.0f, 0.0f}},
-                               45.5e3f, 130e6f, 0.66f, 0.19f, 3.4f, 2.1f, 0.14f, 0.90f, 0.1f};
-constexpr float kPersistentDense = 2.9f;  // the 256 x 256 kernel's start
-constexpr float kTurnedBoth = 1.15f;      // its K loop with both operands turned: twice the LDS reads
+constexpr DenseTimes kBf16Times{FFN_P256, {{1.37f, 0.02f}, {0.787f, 1.05f}, {0.506f, 0.73f}, {0.341f, 0.66f}, {0.273f, 0.73f}, {0.14f, 0.84f}},
+                                153e3f, 10.1e6f, 0.98f, 0.0f, 2.6f, 1.7f, 0.15f, 2.3f, 0.9f};
+constexpr DenseTimes kF32Times{FFN_S128, {{1.328f, 0.52f, 1.67f}, {0.738f, 0.24f, 0.99f}, {0.937f, 0.17f}, {0.521f, 0.19f}, {0.26f, 0.02f}, {0.0f, 0.0f}},
+                               38e3f, 91e6f, 0.54f, 0.25f, 3.4f, 2.3f, 0.083f, 1.36f, 0.5f};
+constexpr float kPersistentDense = 3.2f;  // the 256 x 256 kernel's start
 
 // Estimated time of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
 // turned: B, or both operands, lie the other way round (fp32: after the transposes, which every plan needs, they do not).
@@ -462,7 +461,7 @@ float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, T
   if (slices > 1 && part > kPartBytes) return -1.0f;
   const float stream = (float)((double)(M + R) * K * es + (double)M * N * es) / T.stream;
   const float fetch = (float)GB_ROW_BYTES * ((float)s.brows / mt + (float)s.bm / nt) / T.fetch;
-  const float chunk = std::max(c.chunk * (turned == TURNED_BOTH && bf16 ? kTurnedBoth : 1.0f), fetch);
+  const float chunk = std::max(c.chunk, fetch);  // (turned operands: the same, 440 products)
   float busy = (float)rounds * (KT * chunk + c.fixed);
   if (split) {
     const float all = (float)tiles / kCUs;
@@ -483,7 +482,7 @@ float rows_cost(long long M, long long N, long long K, bool bf16, bool gated) {
   const DenseTimes &T = bf16 ? kBf16Times : kF32Times;
   const int es = bf16 ? 2 : 4;
   const long long blocks = (N + 15) / 16, bytes = ((gated ? 32 : 16) + M) * K * es;
-  constexpr float kAlone = 42e3f, kShared = 30e3f;  // bytes per us of a CU with one workgroup, with several
+  constexpr float kAlone = 37e3f, kShared = 30e3f;  // bytes per us of a CU with one workgroup, with several
   return T.launch + T.rows + (float)((blocks + 255) / 256) * (float)bytes / (blocks > 256 ? kShared : kAlone);
 }
 
