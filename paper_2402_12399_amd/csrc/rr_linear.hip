@@ -188,7 +188,7 @@ __global__ __launch_bounds__(LV_THREADS) void linear_vector_kernel(DenseArgs P) 
       const int n = n0 + v, R = GATED ? 2 * N : N;
       const float g = acc[v][m] + (P.bias ? P.bias[n] : 0.0f);
       const float up = GATED ? acc[v + VR - VN][m] + (P.bias ? P.bias[N + n] : 0.0f) : 0.0f;
-      float y = GATED ? dense_silu<BF16>(g) * up : ACT == RR_ACT_GELU ? gelu_erf(g) : g;
+      float y = GATED ? dense_silu<BF16>(g) * up : ACT == RR_ACT_GELU ? dense_gelu<BF16>(g) : g;
       if (P.pre) {
         store_value<BF16>(P.pre, (size_t)m * R + n, g);
         if (GATED) store_value<BF16>(P.pre, (size_t)m * R + N + n, up);
