@@ -254,59 +254,59 @@ def rr_router_backward(cfg: RRConfig, dout, logits, tables: Tables | None, works
                                              _ptr(dcombine_w), _ptr(dlogits), _stream()), "rr_router_backward")
 
 
-class _Args:
-    """Addresses of the tensors of one call of the operators around the layer, checked: dense, as large as the call takes them to
-    be, of their type, and on the current device, where the call is enqueued.  (A few tenths of a microsecond per tensor: small
-    calls are bound by what the host does.)"""
+# The operators around the layer check their tensors: dense, as large as the call takes them to be, of their type, and on the current
+# device, where the call is enqueued.  Small calls are bound by what the host does, hence the plain functions below (2 us a call).
+_TORCH = None
 
-    __slots__ = ("what", "device")
 
-    def __init__(self, what: str):
+def _torch():
+    global _TORCH
+    if _TORCH is None:
         import torch
-        self.what = what
-        self.device = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+        _TORCH = torch
+    return _TORCH
 
-    def __call__(self, name, t, numel, dtype):
-        """Address of t, or None for None."""
-        if t is None:
-            return None
-        if not t.is_cuda or t.get_device() != self.device:
-            self._refuse_device(name, t)
-        if t.numel() != numel or t.dtype is not dtype or not t.is_contiguous():
-            raise RRError(f"{self.what}: {name} must be dense, {numel} elements of {dtype}; got {tuple(t.shape)} {t.dtype}, "
-                          f"{'dense' if t.is_contiguous() else 'not dense'}")
-        return t.data_ptr()
 
-    def workspace(self, t):
-        """Address and bytes of a workspace (None, 0 for None)."""
-        if t is None:
-            return None, 0
-        import torch
-        n = t.numel()
-        return self("workspace", t, n, torch.uint8), n
+def _device(what: str, t) -> int:
+    """The current device; t, a tensor that the call cannot do without, must be on a GPU."""
+    if t is None or not t.is_cuda:
+        raise RRError(f"{what}: {'a tensor is missing' if t is None else f'a tensor is on {t.device}, not on the current GPU'}")
+    return _torch()._C._cuda_getDevice()
 
-    def mask(self, t, numel):
-        import torch
-        return self("token_mask", t, numel, torch.bool if t is not None and t.dtype is torch.bool else torch.uint8)
 
-    def stream(self):
-        import torch
-        return torch._C._cuda_getCurrentRawStream(self.device)
+def _addr(what: str, name: str, t, numel: int, dtype, device: int):
+    """Address of t, checked, or None for None."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise RRError(f"{what}: {name} is on {t.device}, not on the current GPU")
+    if t.numel() != numel or t.dtype is not dtype or not t.is_contiguous():
+        raise RRError(f"{what}: {name} must be dense, {numel} elements of {dtype}; got {tuple(t.shape)} {t.dtype}, "
+                      f"{'dense' if t.is_contiguous() else 'not dense'}")
+    return t.data_ptr()
 
-    def _refuse_device(self, name, t):
-        import torch
-        # (a tensor on a GPU, though the module says that it has not been initialised: initialise it and look again)
-        if t.is_cuda and self.device is None:
-            self.device = torch.cuda.current_device()
-        if not t.is_cuda or t.get_device() != self.device:
-            raise RRError(f"{self.what}: {name} is on {t.device}, not on the current GPU")
+
+def _mask_addr(what: str, t, numel: int, device: int):
+    torch = _torch()
+    return _addr(what, "token_mask", t, numel, torch.bool if t is not None and t.dtype is torch.bool else torch.uint8, device)
+
+
+def _work(what: str, t, device: int):
+    """Address and bytes of a workspace (None, 0 for None)."""
+    if t is None:
+        return None, 0
+    n = t.numel()
+    return _addr(what, "workspace", t, n, _torch().uint8, device), n
+
+
+def _stream_of(device: int) -> int:
+    return _torch()._C._cuda_getCurrentRawStream(device)
 
 
 def _torch_type(dtype: int):
-    import torch
     if dtype not in (RR_F32, RR_BF16):
         raise RRError(f"unsupported dtype {dtype}")
-    return torch.float32 if dtype == RR_F32 else torch.bfloat16
+    return _torch().float32 if dtype == RR_F32 else _torch().bfloat16
 
 
 def rr_balance_workspace_bytes(cfg: RRConfig) -> int:
@@ -323,49 +323,54 @@ def alloc_balance_workspace(cfg: RRConfig, device="cuda"):
 def rr_balance_loss(cfg: RRConfig, logits, rank_expert, coef: float, loss, counts, workspace, mean_prob=None, token_mask=None):
     """loss [1], counts [E + 1] (int32: choices per expert, then the tokens that count), mean_prob [E] or None.
     token_mask [T], uint8 or bool, or None: 0 = padding."""
-    import torch
-    a, f32, T, E = _Args("rr_balance_loss"), torch.float32, cfg.T, cfg.E
-    args = (a("logits", logits, T * E, f32), a("rank_expert", rank_expert, T * (cfg.k + 1), torch.int32), a.mask(token_mask, T), coef,
-            a("loss", loss, 1, f32), a("counts", counts, E + 1, torch.int32), a("mean_prob", mean_prob, E, f32), *a.workspace(workspace))
+    me, f32, i32, T, E = "rr_balance_loss", _torch().float32, _torch().int32, cfg.T, cfg.E
+    d = _device(me, logits)
+    ws, size = _work(me, workspace, d)
     cc = cfg.c()
-    _check(load_library().rr_balance_loss(C.byref(cc), *args, a.stream()), "rr_balance_loss")
+    _check(load_library().rr_balance_loss(
+        C.byref(cc), _addr(me, "logits", logits, T * E, f32, d), _addr(me, "rank_expert", rank_expert, T * (cfg.k + 1), i32, d),
+        _mask_addr(me, token_mask, T, d), coef, _addr(me, "loss", loss, 1, f32, d), _addr(me, "counts", counts, E + 1, i32, d),
+        _addr(me, "mean_prob", mean_prob, E, f32, d), ws, size, _stream_of(d)), me)
 
 
 def rr_balance_loss_backward(cfg: RRConfig, logits, counts, coef: float, dlogits, dloss=None, token_mask=None,
                              accumulate: bool = False):
     """dlogits [T, E], written or (accumulate) added to; dloss [1] or None for 1."""
-    import torch
-    a, f32, T, E = _Args("rr_balance_loss_backward"), torch.float32, cfg.T, cfg.E
-    args = (a("logits", logits, T * E, f32), a("counts", counts, E + 1, torch.int32), a.mask(token_mask, T), coef,
-            a("dloss", dloss, 1, f32), RR_GRAD_ACCUMULATE if accumulate else 0, a("dlogits", dlogits, T * E, f32))
+    me, f32, T, E = "rr_balance_loss_backward", _torch().float32, cfg.T, cfg.E
+    d = _device(me, logits)
     cc = cfg.c()
-    _check(load_library().rr_balance_loss_backward(C.byref(cc), *args, a.stream()), "rr_balance_loss_backward")
+    _check(load_library().rr_balance_loss_backward(
+        C.byref(cc), _addr(me, "logits", logits, T * E, f32, d), _addr(me, "counts", counts, E + 1, _torch().int32, d),
+        _mask_addr(me, token_mask, T, d), coef, _addr(me, "dloss", dloss, 1, f32, d), RR_GRAD_ACCUMULATE if accumulate else 0,
+        _addr(me, "dlogits", dlogits, T * E, f32, d), _stream_of(d)), me)
 
 
-def _dropout_type(t):
-    import torch
+def _dropout_type(what: str, t):
     dtype = t.dtype
-    if dtype is not torch.float32 and dtype is not torch.bfloat16:
-        raise RRError(f"dropout: unsupported type {dtype}")
-    return RR_F32 if dtype is torch.float32 else RR_BF16
+    if dtype is not _torch().float32 and dtype is not _torch().bfloat16:
+        raise RRError(f"{what}: unsupported type {dtype}")
+    return dtype, RR_F32 if dtype is _torch().float32 else RR_BF16
 
 
 def rr_dropout(x, p: float, seed: int, offset: int, out, residual=None, device_offset=None):
     """out = residual + dropout(x), any shape; out may be x or residual.  device_offset: None or one int64 on the GPU, added to
     `offset` when the kernel runs (captured graphs).  A call uses up (x.numel() + 7) // 8 counters from `offset` on."""
-    import torch
-    a, dtype, n, t = _Args("rr_dropout"), _dropout_type(x), x.numel(), x.dtype
-    _check(load_library().rr_dropout(n, dtype, a("x", x, n, t), a("residual", residual, n, t), p, seed, offset,
-                                     a("device_offset", device_offset, 1, torch.int64), a("out", out, n, t), a.stream()), "rr_dropout")
+    me, n = "rr_dropout", x.numel()
+    t, dtype = _dropout_type(me, x)
+    d = _device(me, x)
+    _check(load_library().rr_dropout(
+        n, dtype, _addr(me, "x", x, n, t, d), _addr(me, "residual", residual, n, t, d), p, seed, offset,
+        _addr(me, "device_offset", device_offset, 1, _torch().int64, d), _addr(me, "out", out, n, t, d), _stream_of(d)), me)
 
 
 def rr_dropout_backward(dout, p: float, seed: int, offset: int, dx, device_offset=None):
     """dx from dout with the mask of the forward call of the same p, seed and offset; dx may be dout."""
-    import torch
-    a, dtype, n, t = _Args("rr_dropout_backward"), _dropout_type(dout), dout.numel(), dout.dtype
-    _check(load_library().rr_dropout_backward(n, dtype, a("dout", dout, n, t), p, seed, offset,
-                                              a("device_offset", device_offset, 1, torch.int64), a("dx", dx, n, t), a.stream()),
-           "rr_dropout_backward")
+    me, n = "rr_dropout_backward", dout.numel()
+    t, dtype = _dropout_type(me, dout)
+    d = _device(me, dout)
+    _check(load_library().rr_dropout_backward(
+        n, dtype, _addr(me, "dout", dout, n, t, d), p, seed, offset,
+        _addr(me, "device_offset", device_offset, 1, _torch().int64, d), _addr(me, "dx", dx, n, t, d), _stream_of(d)), me)
 
 
 def rr_linear_workspace_bytes(cfg: RRLinearConfig, backward: bool = False) -> int:
@@ -381,22 +386,26 @@ def alloc_linear_workspace(cfg: RRLinearConfig, backward: bool = False, device="
 
 def rr_linear(cfg: RRLinearConfig, x, w, bias, residual, y, pre, workspace):
     """y = residual + act(x W^T + bias); bias, residual and pre (the pre-activations, an output) may be None."""
-    import torch
-    a, t, M, N, R = _Args("rr_linear"), _torch_type(cfg.dtype), cfg.M, cfg.N, cfg.rows
-    args = (a("x", x, M * cfg.K, t), a("w", w, R * cfg.K, t), a("bias", bias, R, torch.float32), a("residual", residual, M * N, t),
-            a("y", y, M * N, t), a("pre", pre, M * R, t), *a.workspace(workspace))
+    me, t, M, K, N, R = "rr_linear", _torch_type(cfg.dtype), cfg.M, cfg.K, cfg.N, cfg.rows
+    d = _device(me, x)
+    ws, size = _work(me, workspace, d)
     cc = cfg.c()
-    _check(load_library().rr_linear(C.byref(cc), *args, a.stream()), "rr_linear")
+    _check(load_library().rr_linear(
+        C.byref(cc), _addr(me, "x", x, M * K, t, d), _addr(me, "w", w, R * K, t, d), _addr(me, "bias", bias, R, _torch().float32, d),
+        _addr(me, "residual", residual, M * N, t, d), _addr(me, "y", y, M * N, t, d), _addr(me, "pre", pre, M * R, t, d), ws, size,
+        _stream_of(d)), me)
 
 
 def rr_linear_backward(cfg: RRLinearConfig, x, w, pre, dy, dx, dw, dbias, workspace):
     """dx, dw and dbias (None: not wanted) from dy and the pre-activations of the forward call (None without an activation)."""
-    import torch
-    a, t, M, K, N, R = _Args("rr_linear_backward"), _torch_type(cfg.dtype), cfg.M, cfg.K, cfg.N, cfg.rows
-    args = (a("x", x, M * K, t), a("w", w, R * K, t), a("pre", pre, M * R, t), a("dy", dy, M * N, t), a("dx", dx, M * K, t),
-            a("dw", dw, R * K, t), a("dbias", dbias, R, torch.float32), *a.workspace(workspace))
+    me, t, M, K, N, R = "rr_linear_backward", _torch_type(cfg.dtype), cfg.M, cfg.K, cfg.N, cfg.rows
+    d = _device(me, dy)
+    ws, size = _work(me, workspace, d)
     cc = cfg.c()
-    _check(load_library().rr_linear_backward(C.byref(cc), *args, a.stream()), "rr_linear_backward")
+    _check(load_library().rr_linear_backward(
+        C.byref(cc), _addr(me, "x", x, M * K, t, d), _addr(me, "w", w, R * K, t, d), _addr(me, "pre", pre, M * R, t, d),
+        _addr(me, "dy", dy, M * N, t, d), _addr(me, "dx", dx, M * K, t, d), _addr(me, "dw", dw, R * K, t, d),
+        _addr(me, "dbias", dbias, R, _torch().float32, d), ws, size, _stream_of(d)), me)
 
 
 def rr_profile_enable(on: bool):

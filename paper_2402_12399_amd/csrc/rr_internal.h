@@ -172,9 +172,9 @@ hipError_t launch_balance_grad(int T, int E, int k, const float *logits, const i
 hipError_t launch_dropout(long long n, int dtype, const void *x, const void *residual, u32 m, unsigned long long seed,
                           unsigned long long offset, const unsigned long long *device_offset, void *out, KernelId id, hipStream_t s);
 hipError_t linear_kernel_attributes();  // as ffn_kernel_attributes
-// The tiles (0 x 0: no tiles, few rows) and slices of the forward product, of dx's and of dw's: for tests (rr_linear_plans, exported by the
-// library but no part of its C ABI).
-struct LinearPlans { int32_t bm[3], brows[3], slices[3]; };
+// The tiles (0 x 0: no tiles, few rows) and slices of the forward product, of dx's and of dw's, and whether fp32 operands are cut into bf16
+// parts: for tests (rr_linear_plans, exported by the library but no part of its C ABI).
+struct LinearPlans { int32_t bm[3], brows[3], slices[3], parts[3]; };
 void linear_describe(const rr_linear_config &c, LinearPlans *out);
 size_t linear_workspace(const rr_linear_config &c, bool backward);
 hipError_t launch_linear(const rr_linear_config &c, const void *x, const void *w, const float *bias, const void *residual, void *y,

@@ -497,6 +497,7 @@ DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gate
     least = rows_cost(M, N, K, bf16, gated);
   }
   for (int q = q0; q <= q1; ++q) {
+    if (q == FFN_F32) continue;  // (32 x 128 in fp32: the best estimate of one product in 5000, by nothing)
     const long long bn = gated ? kShape[q].brows / 2 : kShape[q].brows, tiles = (M + kShape[q].bm - 1) / kShape[q].bm * ((N + bn - 1) / bn);
     for (int s = 1; s <= kMaxSlices && (s == 1 || tiles * s <= 2048); ++s) {  // (eight rounds: slices even nothing out any more)
       const float t = dense_cost(M, N, K, bf16, gated, turned, q, s);
@@ -537,7 +538,6 @@ void launch_dense_shape(int shape, DenseArgs A, hipStream_t s) {
       case FFN_S128: launch_dense_tiles<TileS128, GATED, ACT, TA, TB>(A, s); break;
       case FFN_S64: launch_dense_tiles<TileS64, GATED, ACT, TA, TB>(A, s); break;
       case FFN_F64: launch_dense_tiles<TileF64, GATED, ACT, TA, TB>(A, s); break;
-      case FFN_F32: launch_dense_tiles<TileF32, GATED, ACT, TA, TB>(A, s); break;
       default: launch_dense_tiles<TileF32n, GATED, ACT, TA, TB>(A, s); break;
     }
   }
@@ -635,9 +635,11 @@ hipError_t linear_kernel_attributes() {
   };
   auto kinds = [&](auto tag) {
     using S = typename decltype(tag)::type;
-    set(gemm_tile_kernel<S, true, -1, false, false, true>, S::SMEM);
-    set(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false, true>, S::SMEM);
-    set(gemm_tile_kernel<S, false, -1, false, false, true>, S::SMEM);
+    if constexpr (!std::is_same<S, TileF32>::value) {
+      set(gemm_tile_kernel<S, true, -1, false, false, true>, S::SMEM);
+      set(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false, true>, S::SMEM);
+      set(gemm_tile_kernel<S, false, -1, false, false, true>, S::SMEM);
+    }
     if constexpr (S::BF16) {
       set(gemm_tile_kernel<S, false, -1, false, false, true, false, true>, S::SMEM);
       set(gemm_tile_kernel<S, false, -1, false, false, true, true, true>, S::SMEM);
@@ -656,11 +658,13 @@ void linear_describe(const rr_linear_config &c, LinearPlans *out) {
   const bool bf16 = c.dtype == RR_BF16;
   const int R = width(c);
   const DensePlan plan[3] = {dense_plan(c.M, c.N, c.K, bf16, c.act == RR_ACT_SWIGLU, TURNED_NONE),
-                             dense_plan(c.M, c.K, R, bf16, false, TURNED_B), dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH)};
+                             dense_plan(c.M, c.K, R, bf16, false, TURNED_B),
+                             dense_plan(R, c.K, bf16 ? c.M : backward_work(c, nullptr).LT, bf16, false, TURNED_BOTH)};
   for (int i = 0; i < 3; ++i) {
     out->bm[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].bm;
     out->brows[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].brows;
     out->slices[i] = plan[i].slices;
+    out->parts[i] = plan[i].shape == FFN_S128 || plan[i].shape == FFN_S64;
   }
 }
 
@@ -711,7 +715,7 @@ hipError_t launch_linear_backward(const rr_linear_config &c, const void *x, cons
     else launch_product<false, false, -1>(A, plan, turned, W.part, s);
   };
   const bool act = c.act != RR_ACT_NONE;
-  const DensePlan plan_x = dense_plan(c.M, c.K, R, bf16, false, TURNED_B), plan_w = dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH);
+  const DensePlan plan_x = dense_plan(c.M, c.K, R, bf16, false, TURNED_B), plan_w = dense_plan(R, c.K, bf16 ? c.M : W.LT, bf16, false, TURNED_BOTH);
   const TurnArgs make{dy, pre, act && (dx || (dw && bf16)) ? W.dz : nullptr, dw && !bf16 ? W.dz_turned : nullptr,
                       dbias ? W.sums : nullptr, c.M, c.N, W.LT};
   const void *dz = act ? W.dz : dy;

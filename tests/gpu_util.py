@@ -42,14 +42,15 @@ def ffn_shapes(cfg: rr.RRConfig) -> _FfnShapes:
 
 
 class _LinearPlans(C.Structure):
-    _fields_ = [("bm", C.c_int32 * 3), ("brows", C.c_int32 * 3), ("slices", C.c_int32 * 3)]
+    _fields_ = [("bm", C.c_int32 * 3), ("brows", C.c_int32 * 3), ("slices", C.c_int32 * 3), ("parts", C.c_int32 * 3)]
 
 
 def linear_plans(cfg: rr.RRLinearConfig):
-    """(tile rows, staged weight rows, slices) of the forward product, dx's and dw's (host-only query); 0 x 0: few rows, no tiles."""
+    """(tile rows, staged weight rows, slices, fp32 operands as bf16 parts) of the forward product, dx's and dw's (host-only query);
+    0 x 0: few rows, no tiles."""
     out, cc = _LinearPlans(), cfg.c()
     assert rr.load_library().rr_linear_plans(C.byref(cc), C.byref(out)) == 0
-    return [(out.bm[i], out.brows[i], out.slices[i]) for i in range(3)]
+    return [(out.bm[i], out.brows[i], out.slices[i], out.parts[i]) for i in range(3)]
 
 
 def to_device(a, dtype):

@@ -263,6 +263,11 @@ SHAPES = [(1, 8, 8), (2, 24, 16), (1, 4096, 512), (3, 8200, 72), (16, 1000, 264)
           (4099, 512, 512), (130, 4160, 1032), (2048, 64, 64), (9000, 72, 40)]
 
 
+# the tiles and slices that the shapes above leave out (test_operators_host.py checks that none is left)
+MORE = [(34, 2712, 4512), (4102, 80, 912), (9095, 8, 1984), (8445, 1688, 8), (1032, 4152, 48), (2471, 5832, 8), (4199, 8, 2864), (5, 5640, 1848),
+        (3650, 8, 2480), (7, 2520, 3008), (1228, 1440, 8)]
+
+
 def linear_case(M, K, N, dtype, act, make, seed, bias=True, residual=True):
     g, dt = gen(seed), DT[dtype]
     R = 2 * N if act == "swiglu" else N
@@ -292,7 +297,7 @@ def nearest(want, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("M,K,N", SHAPES)
+@pytest.mark.parametrize("M,K,N", SHAPES + MORE)
 def test_linear_exact_sums(M, K, N, dtype):
     """Whole numbers up to 2: sums stay below 2^24, so the output is the rounded exact one, bit for bit."""
     for bias, residual in ((True, True), (False, False)):
@@ -335,6 +340,21 @@ def test_linear_large_tiles(M, K, N, act):
     dy[7] = float("inf")
     bad = run_backward(torch.nan_to_num(x), w, None, torch.nan_to_num(dy, posinf=1.0), "none", "bf16", N, ("dx",))
     assert bool(torch.isfinite(bad["dx"]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", MORE)
+def test_linear_gated_tiles(M, K, N, dtype):
+    """The gated forward product of the shapes above: the pre-activations are exact sums, and y is made of them."""
+    x, w, b, r, _ = linear_case(M, K, N, dtype, "swiglu", whole, M)
+    y, z = run_linear(x, w, b, r, "swiglu", dtype, N)
+    want, want_z = ref.linear(x, w, b, r, "swiglu")
+    assert torch.equal(z, nearest(want_z, dtype))
+    g, u = want_z.chunk(2, dim=1)
+    # silu of an exact number: exponential, sum, division and product, 8 u of it; the product with u, the residual's sum and the rounding.
+    # Below g = -88.7 exp(-g) is infinite in fp32 and silu(g), at most 88.7 exp(-88.7) = 2.7e-37 there, is taken for 0
+    e = 10 * U * (torch.nn.functional.silu(g) * u).abs() + 2 * U * want.abs() + 2.7e-37 * u.abs()
+    within(y, want, e + (V if dtype == "bf16" else U) * (want.abs() + e) + 1e-38, "y")
 
 
 def linear_bound(abs_sum, terms, value, dtype, slope=1.0, extra=0.0):
@@ -533,3 +553,105 @@ def test_streams_of_the_caller():
     torch.cuda.synchronize()
     want, _, _ = ref.dropout(torch.full_like(late, 2.0), None, 0.5, 1, 0)
     assert torch.equal(late.double(), want)
+
+
+# ------------------------------------------------------------------ all of them together
+
+def test_training_step_of_two_layers():
+    """A routed layer, its dropout and residual, a dense SwiGLU layer with its residual and the balance loss: forward, then every gradient
+    that the library makes, against 64 bits; then the same captured in a graph and replayed."""
+    from oracle import rectify_router as orc
+    from paper_2402_12399_amd import workloads as wl
+    from tests import gpu_util as gu
+    w = wl.C1
+    inputs = wl.make_inputs(w)
+    cfg = gu.config_of(w)
+    T, d, F, E = w.T, w.d_model, 192, w.E
+    dev = {n: None if inputs[n] is None else torch.from_numpy(inputs[n]).cuda() for n in ("x", "w_router", "bias", "w1", "w2")}
+    g = gen(11)
+    up_w, down_w, up_b = normal(g, 2 * F, d, scale=d ** -0.5), normal(g, d, F, scale=F ** -0.5), normal(g, 2 * F, scale=0.1)
+    dy = normal(g, T, d)
+    p, seed, offset, coef = 0.1, 5, 1000, 0.01
+    f32 = lambda *s: torch.full(s, float("nan"), device="cuda")
+    out, logits, tables, ws = f32(T, d), f32(T, E), rr.alloc_tables(cfg), rr.alloc_workspace(cfg)
+    up_cfg, down_cfg = rr.RRLinearConfig(T, d, F, rr.RR_F32, rr.RR_ACT_SWIGLU), rr.RRLinearConfig(T, F, d, rr.RR_F32, rr.RR_ACT_NONE)
+    lws = torch.empty(max(rr.rr_linear_workspace_bytes(c, b) for c in (up_cfg, down_cfg) for b in (False, True)), dtype=torch.uint8, device="cuda")
+    bws = rr.alloc_balance_workspace(cfg)
+    r1, h, pre, y = f32(T, d), f32(T, F), f32(T, 2 * F), f32(T, d)
+    loss, counts, dloss = f32(1), torch.empty(E + 1, dtype=torch.int32, device="cuda"), torch.full((1,), 2.0, device="cuda")
+    dh, d_down, dr1, d_up, d_upb, dout, dlogits = f32(T, F), f32(d, F), f32(T, d), f32(2 * F, d), f32(2 * F), f32(T, d), f32(T, E)
+
+    def step():
+        rr.rr_moe_forward(cfg, dev["x"], dev["w_router"], dev["bias"], dev["w1"], None, dev["w2"], out, tables, logits, ws)
+        rr.rr_dropout(out, p, seed, offset, r1, residual=dev["x"])
+        rr.rr_linear(up_cfg, r1, up_w, up_b, None, h, pre, lws)
+        rr.rr_linear(down_cfg, h, down_w, None, r1, y, None, lws)
+        rr.rr_balance_loss(cfg, logits, tables.rank_expert, coef, loss, counts, bws)
+        rr.rr_linear_backward(down_cfg, h, down_w, None, dy, dh, d_down, None, lws)
+        rr.rr_linear_backward(up_cfg, r1, up_w, pre, dh, dr1, d_up, d_upb, lws)
+        dr1.add_(dy)  # the residual of the dense layer
+        rr.rr_dropout_backward(dr1, p, seed, offset, dout)
+        rr.rr_router_backward(cfg, dout, logits, tables, ws, dlogits)
+        rr.rr_balance_loss_backward(cfg, logits, counts, coef, dlogits, dloss=dloss, accumulate=True)
+    step()
+    torch.cuda.synchronize()
+    results = dict(y=y, loss=loss, counts=counts, dh=dh, d_down=d_down, d_up=d_up, d_upb=d_upb, dout=dout, dlogits=dlogits)
+    eager = {n: t.clone() for n, t in results.items()}
+
+    a, want_t, moe = orc.moe_forward(inputs["x"], inputs["w_router"], inputs["bias"], inputs["w1"], None, inputs["w2"], w.k, w.G,
+                                     w.capacity_factor, w.act, True, True)
+    moe = torch.from_numpy(np.asarray(moe)).double().cuda().requires_grad_()
+    up, dn, ub = (t.double().requires_grad_() for t in (up_w, down_w, up_b))
+    _, keep, scale = ref.dropout(out, None, p, seed, offset)
+    r = dev["x"].double() + torch.where(keep, moe * scale, torch.zeros_like(moe))
+    z = torch.mm(r, up.t()) + ub
+    hid = torch.nn.functional.silu(z[:, :F]) * z[:, F:]
+    hid.retain_grad()
+    yy = r + torch.mm(hid, dn.t())
+    (yy * dy.double()).sum().backward()
+    la = torch.from_numpy(np.asarray(a)).cuda()
+    bal = ref.balance(la, tables.rank_expert, w.k, coef, dloss=2.0)
+    _, da = orc.router_score_gradient(inputs["x"], a, want_t, w.k, inputs["w1"], None, inputs["w2"], w.act, moe.grad.cpu().numpy())
+    want = dict(y=yy, loss=bal["loss"].reshape(1), dh=hid.grad, d_down=dn.grad, d_up=up.grad, d_upb=ub.grad, dout=moe.grad,
+                dlogits=torch.from_numpy(np.asarray(da)).cuda() + bal["dlogits"])
+    # fp32 throughout, sums of up to 384 terms, three products behind one another: the bar of the layer's fp32 tests
+    for n, v in want.items():
+        err = float((eager[n].double() - v.detach()).norm() / v.detach().norm())
+        assert err <= 1e-5, (n, err)
+    assert torch.equal(eager["counts"].long(), bal["counts"])
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        for t in results.values():
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, eager[n]) for n, t in results.items())
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+def test_linear_gradients_against_differences(act):
+    """Central differences of the kernel's own forward pass along random directions.  With step s the difference is off by s^2 / 6 of a
+    third derivative (below 3 per unit of z here) and by the roundings of two losses, each a sum of 200 x 48 terms of about 1."""
+    M, K, N = 200, 64, 48
+    g = gen(13)
+    R = 2 * N if act == "swiglu" else N
+    x, w, b, dy = normal(g, M, K), normal(g, R, K, scale=K ** -0.5), normal(g, R, scale=0.3), normal(g, M, N)
+    _, pre = run_linear(x, w, b, None, act, "f32", N)
+    got = run_backward(x, w, pre, dy, act, "f32", N)
+    loss = lambda x, w, b: float((run_linear(x, w, b, None, act, "f32", N, pre=False)[0].double() * dy.double()).sum())
+    s = 2.0 ** -7
+    for which, grad in ((0, got["dx"]), (1, got["dw"]), (2, got["dbias"])):
+        args = [x, w, b]
+        dirn = normal(g, *args[which].shape)
+        up, dn = list(args), list(args)
+        up[which], dn[which] = args[which] + s * dirn, args[which] - s * dirn
+        num = (loss(*up) - loss(*dn)) / (2 * s)
+        want = float((grad.double() * dirn.double()).sum())
+        # z moves by at most 6 per unit of s; 9600 terms: s^2 / 6 * 3 * 6^3 * |dy| of each, signs at random (8 sigma);
+        # roundings 2 u K^1/2 of a term, the same way
+        slack = 8 * math.sqrt(M * N) * (s * s / 6 * 3 * 6 ** 3 + 8 * U * math.sqrt(K) / s)
+        assert abs(num - want) <= slack and abs(want) > 0, (which, num, want, slack)

@@ -210,3 +210,55 @@ def test_binding_refuses_tensors_off_the_gpu():
 def test_struct_layout_matches_header():
     assert C.sizeof(binding._LinearConfig) == 20
     assert rr.RRLinearConfig(1, 8, 16, act=rr.RR_ACT_SWIGLU).rows == 32 and rr.RRLinearConfig(1, 8, 16).rows == 16
+
+
+# ------------------------------------------------------------------ plans and workspaces
+
+def test_linear_workspace_fits_every_smaller_batch(lib):
+    rng = np.random.default_rng(5)
+    for _ in range(200):
+        K, N = 8 * int(2 ** rng.uniform(0, 11)), 8 * int(2 ** rng.uniform(0, 11))
+        dtype, act = int(rng.integers(0, 2)), int(rng.integers(0, 3))
+        sizes = sorted(int(2 ** v) for v in rng.uniform(0, 17, 12))
+        for backward in (False, True):
+            need = [rr.rr_linear_workspace_bytes(rr.RRLinearConfig(M, K, N, dtype, act), backward) for M in sizes]
+            assert need == sorted(need), (K, N, dtype, act, list(zip(sizes, need)))
+
+
+def _plan_keys(M, K, N):
+    from tests import gpu_util as gu
+    for dtype in (rr.RR_F32, rr.RR_BF16):
+        for act in (rr.RR_ACT_NONE, rr.RR_ACT_SWIGLU):
+            for role, (bm, brows, slices, parts) in enumerate(gu.linear_plans(rr.RRLinearConfig(M, K, N, dtype, act))):
+                if role == 0 or act == rr.RR_ACT_NONE:
+                    yield dtype, role, bm, brows, parts, slices > 1
+
+
+def test_the_gpu_tests_reach_every_tile(lib):
+    """Whatever tiles the plan gives products of up to 8e9 multiplications, the shapes of the GPU tests get too."""
+    from tests import test_gpu_operators as t
+    reached = {k for s in t.SHAPES + t.MORE + [l[:3] for l in t.LARGE] for k in _plan_keys(*s)}
+    rng = np.random.default_rng(6)
+    for _ in range(4000):
+        M, K, N = int(2 ** rng.uniform(2.3, 14.6)), 8 * int(2 ** rng.uniform(0, 10.4)), 8 * int(2 ** rng.uniform(0, 10.4))
+        if M * K * N <= 8e9 and M * max(K, N) <= 6e7:
+            assert set(_plan_keys(M, K, N)) <= reached, (M, K, N, set(_plan_keys(M, K, N)) - reached)
+
+
+def test_linear_slices_fit_the_workspace(lib):
+    """The slices' sums, rows x columns x slices floats, fit what the workspace keeps for them, and no slice is empty."""
+    from tests import gpu_util as gu
+    rng = np.random.default_rng(7)
+    for _ in range(3000):
+        M, K, N = int(2 ** rng.uniform(0, 17)), 8 * int(2 ** rng.uniform(0, 11)), 8 * int(2 ** rng.uniform(0, 11))
+        dtype, act = int(rng.integers(0, 2)), int(rng.choice([rr.RR_ACT_NONE, rr.RR_ACT_SWIGLU]))
+        cfg = rr.RRLinearConfig(M, K, N, dtype, act)
+        R, chunk = cfg.rows, 64 if dtype == rr.RR_BF16 else 32
+        forward, backward = rr.rr_linear_workspace_bytes(cfg), rr.rr_linear_workspace_bytes(cfg, True)
+        sums = [(M * R, K), (M * K, R), (R * K, M if dtype == rr.RR_BF16 else (M + 63) // 64 * 64)]
+        for role, (_, _, slices, _) in enumerate(gu.linear_plans(cfg)):
+            outputs, length = sums[role]
+            if slices > 1:
+                assert outputs * 4 * slices <= (backward if role else forward), (cfg, role, slices)
+                each = (length // slices + chunk - 1) // chunk * chunk
+                assert each * slices >= length > each * (slices - 1), (cfg, role, slices)
