@@ -1,6 +1,6 @@
 // Load-balance loss of the router, per-expert counts, and the gradient of the scores:
 //   f_e = c_e / (k n),  P_e = (1/n) sum_t p_te,  loss = coef E sum_e f_e P_e,
-//   dL/da_te = dloss coef E / n  p_te (f_e - sum_j f_j p_tj),   p_t = softmax(a_t) over all experts, n counted tokens.
+//   dL/da_te = dloss coef E / n  p_te (f_e - sum_j f_j p_tj),  p_t = softmax(a_t) over all experts, n counted tokens.
 //
 // LANES lanes share a token's row, four experts each, so that a wave reads 64 / LANES rows at once; maximum and sum go over
 // those lanes by shuffles.  A lane sums its four experts' probabilities over its rows in 64 bits and never touches memory
@@ -241,12 +241,20 @@ __global__ __launch_bounds__(BG_THREADS) void balance_grad_kernel(BalanceGradArg
   const int n = A.counts[E];
   const float each = n > 0 ? 1.0f / ((float)A.k * (float)n) : 0.0f;
   const float scale = n > 0 ? (A.dloss ? *A.dloss : 1.0f) * A.coef * (float)E / (float)n : 0.0f;
-  float f[4];
+  // f_e less the mean of all: the mean falls out of f_e - sum_j f_j p_tj, as the p_tj add up to 1, and with it goes most of what would
+  // cancel where the experts are nearly balanced (all alike: zeros, not rounding errors).  Differences of whole numbers are exact.
+  int32_t count[4], sum = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int e = expert_of<LANES, VEC>(lane, j);
-    f[j] = e < E ? (float)A.counts[e] * each : 0.0f;
+    count[j] = e < E ? A.counts[e] : 0;
+    sum += count[j];
   }
+#pragma unroll
+  for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor(sum, o);
+  float f[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = expert_of<LANES, VEC>(lane, j) < E ? (float)(count[j] - sum / E) * each : 0.0f;
   // from the last row to the first: the loss has just read the last ones, which the last-level cache still holds
   const int step = gridDim.x * WAVES * ROWS;
   for (int t0 = (blockIdx.x * WAVES + w) * ROWS; t0 < A.T; t0 += step) {

@@ -229,6 +229,12 @@ def test_balance_edges():
     check_balance(a, bad, 2, 0.5)
     # all on one expert
     check_balance(a, torch.full_like(ranks, 5), 2, 0.5)
+    # every expert chosen as often as any other: the gradient is zero, and so is what is written
+    for E in (3, 4, 8):
+        a = normal(g, 40, E)
+        rolled = (torch.arange(40, device="cuda")[:, None] + torch.arange(3, device="cuda")) % E
+        _, _, _, grad = run_balance(a[:E * 3], rolled[:E * 3].int(), 2, 0.5)
+        assert not bool(grad.any())
 
 
 @pytest.mark.parametrize("E", [6, 7, 8, 64])
