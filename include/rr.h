@@ -10,6 +10,9 @@
  * (expert j lives on group j / (E/G), token i on group i / (T/G)); the token all-to-all of
  * expert parallelism (Sec. 3) is a permutation in device memory.
  *
+ * Around the layer: the router's balance loss with its gradient (rr_balance_loss*), dropout with the residual sum
+ * (rr_dropout*) and the dense projections of the FFN layers in between (rr_linear*), each with its backward pass.
+ *
  * General conventions
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library allocates no
  *     device memory and keeps no DATA between calls; scratch comes from `workspace` (one entry
@@ -267,12 +270,14 @@ typedef struct rr_linear_config {
   int32_t act;   /* RR_ACT_NONE | RR_ACT_GELU | RR_ACT_SWIGLU             */
 } rr_linear_config;
 
-/* Scratch of rr_linear (backward = 0) or rr_linear_backward (1): a multiple of 256 bytes.  Host function. */
+/* Scratch of rr_linear (backward = 0) or rr_linear_backward (1): a multiple of 256 bytes; what is enough for M rows is enough for
+ * fewer.  Host function. */
 int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, size_t *bytes);
 
 /*   x [M,K], w [R,K], bias [R] fp32 or NULL, residual [M,N] or NULL (may be y itself)
  *   y   [M,N] out
  *   pre [M,R] out or NULL: z, rounded to cfg->dtype, for rr_linear_backward
+ * Outputs overlap neither each other nor an input (but y may be residual).
  * Products are accumulated, and act and the sums made, in fp32; y is rounded once. */
 int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual,
               void *y, void *pre, void *workspace, size_t workspace_bytes, void *stream);
@@ -280,7 +285,8 @@ int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const f
 /* Gradients for dy [M,N]: with dz = dy act'(z) (bf16: rounded to bf16 for the two products)
  *     dx = dz W [M,K],   dw = dz^T x [R,K],   dbias = sum over rows of dz [R] fp32;   the residual's is dy.
  *   pre     the forward call's; ignored with RR_ACT_NONE
- *   dx, dw, dbias   each may be NULL (not all); x is needed for dw only and w for dx only, else NULL is allowed
+ *   dx, dw, dbias   each may be NULL (not all); x is needed for dw only and w for dx only, else NULL is allowed.  None of them may
+ *                   overlap an input
  * x, w, residual, y, pre, dy, dx and dw 16-byte aligned, bias and dbias 4-byte, the workspace 256-byte.  Sums run in a fixed
  * order: results do not change from run to run. */
 int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w, const void *pre, const void *dy,

@@ -1,4 +1,5 @@
-"""Rectify-Router MoE-layer forward (and the router-score gradient of its weights) for AMD MI355X (gfx950).
+"""Rectify-Router MoE-layer forward (and the router-score gradient of its weights) for AMD MI355X (gfx950), and what a model calls
+around it: balance loss, dropout with the residual sum, dense projections, each with its gradient.
 
 The product is the HIP library `librr.so` (C ABI in include/rr.h); `binding` marshals torch
 tensors into it and `workloads` draws seeded synthetic inputs.  There is no CPU fallback: every
