@@ -470,6 +470,104 @@ def test_linear_infinities_and_nan_stay_in_their_rows(M, K, N, dtype):
     assert bool(y[2].isnan().all()) and not bool(torch.isfinite(y[4]).any()) and not bool(torch.isfinite(y[:, 9]).any())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(70, 72, 136), (700, 1000, 264), (1030, 2048, 1544)])
+def test_gradients_keep_nan_and_infinities_apart(M, K, N, dtype):
+    """x[m, k] reaches column k of dw, dy[m, n] row m of dx and row n of dw; all other sums are of whole numbers, exact either way."""
+    x, w, _, _, _ = linear_case(M, K, N, dtype, "none", whole, 7, False, False)
+    dy = whole(gen(8), M, N, dtype=DT[dtype])
+    clean = run_backward(x, w, None, dy, "none", dtype, N, ("dx", "dw"))
+    x[5, 3], dy[7, 2] = float("nan"), float("inf")
+    cfg = rr.RRLinearConfig(M, K, N, rr.RR_F32 if dtype == "f32" else rr.RR_BF16, rr.RR_ACT_NONE)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    rr.rr_linear_backward(cfg, x, w, None, dy, dx, dw, None, rr.alloc_linear_workspace(cfg, True))
+    rows = torch.arange(M, device="cuda") != 7
+    outs, cols = torch.arange(N, device="cuda") != 2, torch.arange(K, device="cuda") != 3
+    assert torch.equal(dx[rows], clean["dx"][rows]) and torch.equal(dw[outs][:, cols], clean["dw"][outs][:, cols])
+    assert not bool(torch.isfinite(dx[7][w[2] != 0]).any()) and bool(dw[:, 3].isnan().all())
+
+
+@pytest.mark.parametrize("M,K,N", [(3, 264, 72), (20, 264, 72), (300, 264, 520), (600, 2048, 264)])
+@pytest.mark.parametrize("ex,ew", [(60, 40), (-100, -20), (-140, 20), (20, -60)])
+def test_linear_f32_keeps_the_whole_range(M, K, N, ex, ew):
+    """Whole numbers times powers of two, subnormal ones among them: sums are exact however the operands are cut."""
+    x, w, _, _, _ = linear_case(M, K, N, "f32", "none", whole, 9, False, False)
+    big, want = x * 2.0 ** ex, torch.mm(x.double(), w.double().t()) * 2.0 ** (ex + ew)
+    y, _ = run_linear(big, w * 2.0 ** ew, None, None, "none", "f32", N, pre=False)
+    assert torch.equal(y.double(), want)
+
+
+def test_linear_bias_needs_four_byte_alignment_only():
+    for M, act in ((2, "none"), (40, "gelu"), (300, "swiglu")):
+        x, w, b, r, R = linear_case(M, 264, 136, "bf16", act, normal, 10)
+        y, _ = run_linear(x, w, b, r, act, "bf16", 136)
+        shifted = torch.empty(R + 1, device="cuda")
+        shifted[1:] = b
+        again, _ = run_linear(x, w, shifted[1:], r, act, "bf16", 136)
+        assert torch.equal(y, again)
+
+
+# ------------------------------------------------------------------ offsets beyond 32 bits, the longest rows and the most of them
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K,N", [(1 << 21, 1032, 64), (40, 1 << 18, 16), (3, 1 << 18, 16), (40, 16, 1 << 18), (300, 1 << 17, 72)])
+def test_linear_at_the_limits(M, K, N, dtype):
+    """Whole numbers, sums below 2^24: exact.  Of the many rows some are compared, and every sum over them (dw, dbias)."""
+    g, dt = gen(12), DT[dtype]
+    x, w, dy = whole(g, M, K, dtype=dt, top=1), whole(g, N, K, dtype=dt, top=1), whole(g, M, N, dtype=dt, top=1)
+    cfg = rr.RRLinearConfig(M, K, N, rr.RR_F32 if dtype == "f32" else rr.RR_BF16, rr.RR_ACT_NONE)
+    y, dx, dw, db = torch.full((M, N), float("nan"), dtype=dt, device="cuda"), torch.full_like(x, float("nan")), torch.full_like(w, float("nan")), torch.empty(N, device="cuda")
+    rr.rr_linear(cfg, x, w, None, None, y, None, rr.alloc_linear_workspace(cfg))
+    rr.rr_linear_backward(cfg, x, w, None, dy, dx, dw, db, rr.alloc_linear_workspace(cfg, True))
+    some = torch.unique(torch.cat([torch.arange(min(M, 300), device="cuda"), torch.arange(max(0, M - 300), M, device="cuda"),
+                                   torch.randint(0, M, (300,), generator=g, device="cuda")]))
+    assert torch.equal(y[some], nearest(torch.mm(x[some].double(), w.double().t()), dtype))
+    assert torch.equal(dx[some], nearest(torch.mm(dy[some].double(), w.double()), dtype))
+    want = torch.zeros(N, K, dtype=torch.float64, device="cuda")
+    for a in range(0, M, 1 << 17):
+        want += torch.mm(dy[a:a + (1 << 17)].double().t().contiguous(), x[a:a + (1 << 17)].double())
+    assert torch.equal(dw, nearest(want, dtype)) and torch.equal(db.double(), dy.double().sum(dim=0))
+
+
+def test_dropout_beyond_32_bits():
+    n = (1 << 31) + 13
+    x = torch.ones(n, dtype=BF16, device="cuda")
+    out = torch.zeros_like(x)
+    rr.rr_dropout(x, 0.25, 3, 2 ** 63, out, residual=x)
+    for a in (0, (1 << 30) - 8, (1 << 31) - 4096):
+        b = min(n, a + 8192)
+        want, _, _ = ref.dropout(x[a:b], x[a:b], 0.25, 3, 2 ** 63 + a // 8)
+        assert torch.equal(out[a:b], nearest(want, "bf16"))
+
+
+def test_balance_of_the_most_tokens():
+    T, E, k = 1 << 24, 64, 2
+    g = gen(14)
+    a = torch.randn((T, E), generator=g, device="cuda")
+    ranks = torch.randint(0, E, (T, k + 1), generator=g, device="cuda", dtype=torch.int32)
+    cfg = rr.RRConfig(T, 8, 0, E, k, 1, 1.0, rr.RR_F32, rr.RR_ACT_SWIGLU, 0)
+    loss, counts, mean, grad = (torch.empty(s, device="cuda") for s in (1, E + 1, E, a.shape))
+    counts = torch.empty(E + 1, dtype=torch.int32, device="cuda")
+    rr.rr_balance_loss(cfg, a, ranks, 1.0, loss, counts, rr.alloc_balance_workspace(cfg), mean_prob=mean)
+    rr.rr_balance_loss_backward(cfg, a, counts, 1.0, grad)
+    total, want_counts = torch.zeros(E, dtype=torch.float64, device="cuda"), torch.zeros(E, dtype=torch.int64, device="cuda")
+    for t in range(0, T, 1 << 21):
+        total += torch.softmax(a[t:t + (1 << 21)].double(), dim=1).sum(dim=0)
+        want_counts += torch.bincount(ranks[t:t + (1 << 21), :k].reshape(-1).long(), minlength=E)
+    assert torch.equal(counts[:E].long(), want_counts) and int(counts[E]) == T
+    s = float(a.max() - a.min())
+    c = (2 * s + 20) * U
+    within(mean, total / T, c * total / T, "mean_prob")
+    f = want_counts.double() / (k * T)
+    assert abs(float(loss) - float(E * (f * total / T).sum())) <= (c + 4 * U) * float(E * (f * total / T).sum())
+    for t in (0, T // 2 - 1000, T - 4096):
+        p = torch.softmax(a[t:t + 4096].double(), dim=1)
+        pf = (p * f).sum(dim=1, keepdim=True)
+        scale = E / T
+        bound = scale * p * ((c + 8 * U) * (f + pf) + c * (f - pf).abs() + (c + 12 * U) * pf) + 1e-40
+        within(grad[t:t + 4096], scale * p * (f - pf), bound, "dlogits")
+
+
 # ------------------------------------------------------------------ streams, graphs, both calls at once
 
 def _calls():
