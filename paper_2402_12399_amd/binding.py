@@ -62,6 +62,13 @@ class RRConfig:
                        self.dtype, self.act, self.flags)
 
 
+def _no_wrap(cfg, fields: int):
+    """Refuses what the C structure would cut to 32 bits.  `fields`: all of them or-ed together; one that is negative, which may hide
+    others, the library refuses itself."""
+    if fields >> 31 not in (0, -1):
+        raise RRError(f"{cfg}: a field does not fit in 32 bits")
+
+
 @dataclass
 class RRLinearConfig:
     M: int
@@ -76,6 +83,7 @@ class RRLinearConfig:
         return 2 * self.N if self.act == RR_ACT_SWIGLU else self.N
 
     def c(self) -> _LinearConfig:
+        _no_wrap(self, self.M | self.K | self.N | self.dtype | self.act)
         return _LinearConfig(self.M, self.K, self.N, self.dtype, self.act)
 
 
@@ -309,8 +317,13 @@ def _torch_type(dtype: int):
     return _torch().float32 if dtype == RR_F32 else _torch().bfloat16
 
 
+def _balance_config(cfg: RRConfig) -> _Config:
+    _no_wrap(cfg, cfg.T | cfg.E | cfg.k)
+    return cfg.c()
+
+
 def rr_balance_workspace_bytes(cfg: RRConfig) -> int:
-    n, cc = C.c_size_t(0), cfg.c()
+    n, cc = C.c_size_t(0), _balance_config(cfg)
     _check(load_library().rr_balance_workspace_bytes(C.byref(cc), C.byref(n)), "rr_balance_workspace_bytes")
     return int(n.value)
 
@@ -326,7 +339,7 @@ def rr_balance_loss(cfg: RRConfig, logits, rank_expert, coef: float, loss, count
     me, f32, i32, T, E = "rr_balance_loss", _torch().float32, _torch().int32, cfg.T, cfg.E
     d = _device(me, logits)
     ws, size = _work(me, workspace, d)
-    cc = cfg.c()
+    cc = _balance_config(cfg)
     _check(load_library().rr_balance_loss(
         C.byref(cc), _addr(me, "logits", logits, T * E, f32, d), _addr(me, "rank_expert", rank_expert, T * (cfg.k + 1), i32, d),
         _mask_addr(me, token_mask, T, d), coef, _addr(me, "loss", loss, 1, f32, d), _addr(me, "counts", counts, E + 1, i32, d),
@@ -338,7 +351,7 @@ def rr_balance_loss_backward(cfg: RRConfig, logits, counts, coef: float, dlogits
     """dlogits [T, E], written or (accumulate) added to; dloss [1] or None for 1."""
     me, f32, T, E = "rr_balance_loss_backward", _torch().float32, cfg.T, cfg.E
     d = _device(me, logits)
-    cc = cfg.c()
+    cc = _balance_config(cfg)
     _check(load_library().rr_balance_loss_backward(
         C.byref(cc), _addr(me, "logits", logits, T * E, f32, d), _addr(me, "counts", counts, E + 1, _torch().int32, d),
         _mask_addr(me, token_mask, T, d), coef, _addr(me, "dloss", dloss, 1, f32, d), RR_GRAD_ACCUMULATE if accumulate else 0,

@@ -207,6 +207,22 @@ def test_binding_refuses_tensors_off_the_gpu():
         rr.rr_linear(rr.RRLinearConfig(4, 8, 8, 7), f(4, 8), f(8, 8), None, None, f(4, 8), None, None)
 
 
+@pytest.mark.parametrize("kw", [dict(M=(1 << 32) + 16), dict(K=(1 << 32) + 64), dict(N=(1 << 32) + 64), dict(act=(1 << 32) + rr.RR_ACT_SWIGLU),
+                                dict(M=16 - (1 << 32)), dict(dtype=1 << 32)])
+def test_linear_configuration_does_not_wrap(kw):
+    """Sizes and types that 32 bits do not hold are no others."""
+    cfg = rr.RRLinearConfig(**dict(dict(M=16, K=64, N=64), **kw))
+    with pytest.raises(rr.RRError, match="32 bits"):
+        rr.rr_linear_workspace_bytes(cfg)
+
+
+@pytest.mark.parametrize("kw", [dict(T=(1 << 32) + 4), dict(k=(1 << 32) + 2), dict(E=(1 << 32) + 8), dict(T=4 - (1 << 32))])
+def test_balance_configuration_does_not_wrap(kw):
+    cfg = rr.RRConfig(**dict(dict(T=4, d_model=8, d_ff=0, E=4, k=2, G=1, capacity_factor=1.0), **kw))
+    with pytest.raises(rr.RRError, match="32 bits"):
+        rr.rr_balance_workspace_bytes(cfg)
+
+
 def test_struct_layout_matches_header():
     assert C.sizeof(binding._LinearConfig) == 20
     assert rr.RRLinearConfig(1, 8, 16, act=rr.RR_ACT_SWIGLU).rows == 32 and rr.RRLinearConfig(1, 8, 16).rows == 16
