@@ -229,7 +229,7 @@ int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *ra
  *   dloss       [1] fp32 on the device, or NULL for 1
  *   grad_flags  0, or RR_GRAD_ACCUMULATE: added to what dlogits holds (rr_router_backward's, say); rows of tokens that do not
  *               count are then left as they are
- *   dlogits     [T,E] fp32 in/out; not the same memory as logits */
+ *   dlogits     [T,E] fp32 in/out; shares no memory with logits (RR_ERR_INVALID_ARG) */
 #define RR_GRAD_ACCUMULATE 2u
 int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const int32_t *counts, const uint8_t *token_mask,
                              float coef, const float *dloss, uint32_t grad_flags, float *dlogits, void *stream);
@@ -247,7 +247,7 @@ int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const in
  *   p              0 <= p <= 1, taken in steps of 1 / 65536; at p = 1 out is the residual (or 0)
  *   device_offset  NULL, or one uint64 on the device (8-byte aligned) that is added to `offset` when the kernel runs: a captured
  *                  graph then draws another mask in each replay
- *   out            [n]; may be x or residual itself
+ *   out            [n]; may be x or residual itself, but not overlap one of them otherwise (RR_ERR_INVALID_ARG)
  * A dropped element leaves nothing behind, whatever its value (NaN and infinities too).  The sum is made in fp32 and rounded
  * once.  All data pointers 16-byte aligned. */
 int rr_dropout(int64_t n, int32_t dtype, const void *x, const void *residual, float p, uint64_t seed, uint64_t offset,
@@ -277,7 +277,7 @@ int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, siz
 /*   x [M,K], w [R,K], bias [R] fp32 or NULL, residual [M,N] or NULL (may be y itself)
  *   y   [M,N] out
  *   pre [M,R] out or NULL: z, rounded to cfg->dtype, for rr_linear_backward
- * Outputs overlap neither each other nor an input (but y may be residual).
+ * Outputs overlap neither each other nor an input (but y may be residual), or the call is refused (RR_ERR_INVALID_ARG).
  * Products are accumulated, and act and the sums made, in fp32; y is rounded once. */
 int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual,
               void *y, void *pre, void *workspace, size_t workspace_bytes, void *stream);
@@ -286,7 +286,7 @@ int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const f
  *     dx = dz W [M,K],   dw = dz^T x [R,K],   dbias = sum over rows of dz [R] fp32;   the residual's is dy.
  *   pre     the forward call's; ignored with RR_ACT_NONE
  *   dx, dw, dbias   each may be NULL (not all); x is needed for dw only and w for dx only, else NULL is allowed.  None of them may
- *                   overlap an input
+ *                   overlap another or an input that is needed (RR_ERR_INVALID_ARG)
  * x, w, residual, y, pre, dy, dx and dw 16-byte aligned, bias and dbias 4-byte, the workspace 256-byte.  Sums run in a fixed
  * order: results do not change from run to run. */
 int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w, const void *pre, const void *dy,

@@ -205,6 +205,26 @@ static size_t carve(const Dims &D, Use use, void *ws, Work *W) {
 // wise unless the row itself is a multiple of 16 bytes).  NULL (optional arguments) passes.
 static bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+// An operand of the operators around the layer, or nothing (p = NULL).
+struct Span {
+  const void *p;
+  size_t bytes;
+};
+static bool meet(const Span &a, const Span &b) {
+  const uintptr_t i = reinterpret_cast<uintptr_t>(a.p), j = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && i < j + b.bytes && j < i + a.bytes;
+}
+// Whether one of `outs` shares memory with another of them or with one of `ins`.
+template <size_t O, size_t I>
+static bool any_meet(const Span (&outs)[O], const Span (&ins)[I]) {
+  for (size_t i = 0; i < O; ++i) {
+    for (size_t j = 0; j < i; ++j)
+      if (meet(outs[i], outs[j])) return true;
+    for (const Span &in : ins)
+      if (meet(outs[i], in)) return true;
+  }
+  return false;
+}
 static bool tables_aligned(const rr_tables *t) {
   return aligned4(t->rank_expert) && aligned4(t->slot) && aligned4(t->slot_token) && aligned4(t->fill_topk) &&
          aligned4(t->fill_total) && aligned4(t->ir_expert) && aligned4(t->ir_row) && aligned4(t->ir_offset) &&
@@ -413,7 +433,8 @@ int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const in
   Dims D;
   const int rc = make_dims(cfg, false, &D);
   if (rc != RR_OK) return rc;
-  if (!logits || !counts || !dlogits || logits == dlogits || !isfinite(coef)) return RR_ERR_INVALID_ARG;
+  const size_t scores = (size_t)D.T * D.E * 4;
+  if (!logits || !counts || !dlogits || meet({logits, scores}, {dlogits, scores}) || !isfinite(coef)) return RR_ERR_INVALID_ARG;
   if (grad_flags & ~(uint32_t)RR_GRAD_ACCUMULATE) return RR_ERR_INVALID_ARG;
   if (!aligned4(logits) || !aligned4(counts) || !aligned4(dloss) || !aligned4(dlogits)) return RR_ERR_INVALID_ARG;
   const hipError_t e = launch_balance_grad(D.T, D.E, D.k, logits, counts, token_mask, coef, dloss,
@@ -427,6 +448,9 @@ static int dropout(int64_t n, int32_t dtype, const void *x, const void *residual
   if ((dtype != RR_F32 && dtype != RR_BF16) || n > (int64_t)1 << 40) return RR_ERR_UNSUPPORTED;
   if (!aligned16(x) || !aligned16(residual) || !aligned16(out) || (reinterpret_cast<uintptr_t>(device_offset) & 7))
     return RR_ERR_INVALID_ARG;
+  const size_t bytes = (size_t)n * (dtype == RR_BF16 ? 2 : 4);
+  for (const void *in : {x, residual})
+    if (in != out && meet({in, bytes}, {out, bytes})) return RR_ERR_INVALID_ARG;
   const u32 m = (u32)floor(65536.0 * (double)p + 0.5);
   const hipError_t e = launch_dropout(n, dtype, x, residual, m, seed, offset, reinterpret_cast<const unsigned long long *>(device_offset),
                                       out, id, static_cast<hipStream_t>(stream));
@@ -453,6 +477,19 @@ static int check_linear(const rr_linear_config *c) {
   return RR_OK;
 }
 
+// Of the operands of a projection and, as they are of the same sizes, of their gradients.
+struct LinearBytes {
+  size_t x, w, y, z, bias;
+  explicit LinearBytes(const rr_linear_config &c) {
+    const size_t es = c.dtype == RR_BF16 ? 2 : 4, M = c.M, K = c.K, N = c.N, R = c.act == RR_ACT_SWIGLU ? 2 * N : N;
+    x = M * K * es;
+    w = R * K * es;
+    y = M * N * es;
+    z = M * R * es;
+    bias = R * 4;
+  }
+};
+
 int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, size_t *bytes) {
   if (!bytes || (backward != 0 && backward != 1)) return RR_ERR_INVALID_ARG;
   const int rc = check_linear(cfg);
@@ -476,6 +513,9 @@ int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const f
     return RR_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < linear_workspace(*cfg, false))
     return RR_ERR_WORKSPACE;
+  const LinearBytes L(*cfg);
+  if (any_meet({{y, L.y}, {pre, L.z}}, {{x, L.x}, {w, L.w}, {bias, L.bias}, {residual == y ? nullptr : residual, L.y}}))
+    return RR_ERR_INVALID_ARG;
   if (device_setup() < 0) return RR_ERR_HIP;
   const hipError_t e = launch_linear(*cfg, x, w, bias, residual, y, pre, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? RR_OK : RR_ERR_HIP;
@@ -490,6 +530,10 @@ int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w
     return RR_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < linear_workspace(*cfg, true))
     return RR_ERR_WORKSPACE;
+  const LinearBytes L(*cfg);
+  if (any_meet({{dx, L.x}, {dw, L.w}, {dbias, L.bias}},
+               {{dy, L.y}, {dw ? x : nullptr, L.x}, {dx ? w : nullptr, L.w}, {cfg->act != RR_ACT_NONE ? pre : nullptr, L.z}}))
+    return RR_ERR_INVALID_ARG;
   if (device_setup() < 0) return RR_ERR_HIP;
   const hipError_t e = launch_linear_backward(*cfg, x, w, pre, dy, dx, dw, dbias, workspace, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? RR_OK : RR_ERR_HIP;

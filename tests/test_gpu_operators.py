@@ -568,6 +568,32 @@ def test_balance_of_the_most_tokens():
         within(grad[t:t + 4096], scale * p * (f - pf), bound, "dlogits")
 
 
+def test_neighbours_in_one_buffer():
+    """Operands and results that lie next to one another, without a byte between them, are all there is to tell apart."""
+    M, K, N, at = 48, 64, 32, 0
+    store = torch.empty(1 << 16, dtype=BF16, device="cuda")
+
+    def take(*shape):
+        nonlocal at
+        n = math.prod(shape)
+        at += n
+        return store[at - n:at].view(shape)
+    x, y, w, pre, dy, dx, dw = take(M, K), take(M, N), take(2 * N, K), take(M, 2 * N), take(M, N), take(M, K), take(2 * N, K)
+    for t in (x, w, dy):
+        t.copy_(normal(gen(31), *t.shape, dtype=BF16))
+    cfg = rr.RRLinearConfig(M, K, N, rr.RR_BF16, rr.RR_ACT_SWIGLU)
+    rr.rr_linear(cfg, x, w, None, None, y, pre, rr.alloc_linear_workspace(cfg))
+    rr.rr_linear_backward(cfg, x, w, pre, dy, dx, dw, None, rr.alloc_linear_workspace(cfg, True))
+    x, w, dy = x.clone(), w.clone(), dy.clone()
+    apart_y, apart_pre = run_linear(x, w, None, None, "swiglu", "bf16", N)
+    assert torch.equal(apart_y, y) and torch.equal(apart_pre, pre)
+    apart = run_backward(x, w, apart_pre, dy, "swiglu", "bf16", N, ("dx", "dw"))
+    assert torch.equal(apart["dx"], dx) and torch.equal(apart["dw"], dw)
+    a, b = store[:1000], store[1000:2000]
+    rr.rr_dropout(a, 0.5, 1, 2, b)
+    assert torch.equal(b, (lambda o: (rr.rr_dropout(a, 0.5, 1, 2, o), o)[1])(torch.empty_like(a)))
+
+
 # ------------------------------------------------------------------ streams, graphs, both calls at once
 
 def _calls():

@@ -145,6 +145,58 @@ def test_linear_refusals(lib):
         assert backward(**kw) == WORKSPACE, kw
 
 
+def at(byte):
+    return C.c_void_p(0x100000 + byte)
+
+
+def test_linear_outputs_do_not_overlap(lib):
+    """Each pair that may not meet, by as little as 16 bytes (bias: 4); y may be residual, but not a part of it."""
+    M, K, N = 16, 64, 32
+    c = _linear(M=M, K=K, N=N, act=rr.RR_ACT_SWIGLU)
+    x, w, y, z, b = M * K * 2, 2 * N * K * 2, M * N * 2, M * 2 * N * 2, 2 * N * 4
+    gap = 1 << 15
+    size = dict(x=x, w=w, bias=b, residual=y, y=y, pre=z)
+    good = {name: gap * i for i, name in enumerate(size)}
+
+    def forward(**kw):
+        a = {name: at(v) for name, v in dict(good, **kw).items()}
+        return lib.rr_linear(C.byref(c), a["x"], a["w"], a["bias"], a["residual"], a["y"], a["pre"], at(8 * gap), BIG, None)
+    for out in ("y", "pre"):
+        for other in size:
+            if other == out:
+                continue
+            last = 4 if other == "bias" else 16
+            for place in (good[other] - size[out] + 16, good[other] + (size[other] - last) // 16 * 16):
+                assert forward(**{out: place}) == INVALID, (out, other, place)
+            if (out, other) != ("y", "residual"):
+                assert forward(**{out: good[other]}) == INVALID, (out, other)
+    size = dict(x=x, w=w, pre=z, dy=y, dx=x, dw=w, dbias=b)
+    good = {name: gap * i for i, name in enumerate(size)}
+
+    def backward(**kw):
+        a = {name: at(v) for name, v in dict(good, **kw).items()}
+        return lib.rr_linear_backward(C.byref(c), a["x"], a["w"], a["pre"], a["dy"], a["dx"], a["dw"], a["dbias"], at(8 * gap), BIG, None)
+    for out in ("dx", "dw", "dbias"):
+        for other in size:
+            if other != out:
+                for place in (good[other] - size[out] + 16, good[other], good[other] + size[other] - 16):
+                    assert backward(**{out: place}) == INVALID, (out, other, place)
+
+
+def test_dropout_and_balance_outputs_do_not_overlap(lib):
+    gap = 1 << 15
+    for dtype, es in ((rr.RR_F32, 4), (rr.RR_BF16, 2)):
+        n = 1000
+        for place in (-n * es + 16, -16, 16, n * es - 16):
+            assert lib.rr_dropout(n, dtype, at(gap), None, 0.1, 1, 2, None, at(gap + place), None) == INVALID
+            assert lib.rr_dropout(n, dtype, at(gap), at(5 * gap), 0.1, 1, 2, None, at(5 * gap + place), None) == INVALID
+            assert lib.rr_dropout_backward(n, dtype, at(gap), 0.1, 1, 2, None, at(gap + place), None) == INVALID
+    c = rr.RRConfig(T=64, d_model=64, d_ff=0, E=8, k=2, G=2, capacity_factor=1.0).c()
+    for place in (-64 * 8 * 4 + 4, 0, 64 * 8 * 4 - 4):
+        assert lib.rr_balance_loss_backward(C.byref(c), at(gap), at(5 * gap), None, 0.1, None, 0, at(gap + place), None) == INVALID
+        assert lib.rr_balance_loss_backward(C.byref(c), at(gap), at(5 * gap), None, 0.1, None, 2, at(gap + place), None) == INVALID
+
+
 def test_dropout_refusals(lib):
     def call(n=64, dtype=rr.RR_BF16, x=FAKE, residual=None, p=0.1, dev=None, out=FAKE):
         a = lib.rr_dropout(n, dtype, x, residual, p, 1, 2, dev, out, None)
