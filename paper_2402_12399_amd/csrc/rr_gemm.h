@@ -112,6 +112,7 @@ __device__ inline float dense_gelu(float g) {
 constexpr int GB_BK = 64;             // bf16 elements per K chunk = 128 B per LDS row
 constexpr int GB_ROW_BYTES = 128;
 [[maybe_unused]] constexpr u32 BUF_FLAGS = 0x00020000; // raw buffer descriptor word 3 (32-bit data format)
+[[maybe_unused]] constexpr int BUF_STREAM = 2;           // cache policy of a load: not kept for another reader (nontemporal)
 
 struct GemmArgs {
   const void *A;        // [rows, K] dispatched rows; with GATHER: x [T, K]
@@ -896,8 +897,8 @@ struct TileShape {
   static constexpr int STAGE = (BM + BROWS) * (MATH == TILE_SPLIT ? 3 * GB_ROW_BYTES / 2 : GB_ROW_BYTES), SMEM = ST * STAGE;
 };
 
-// ACT: RR_ACT_GELU, RR_ACT_SWIGLU (bf16: with the division), or -1
-template <class S, bool GATED, int ACT, bool GATHER, bool DIRECT, bool DENSE = false, bool TA = false, bool TB = false>
+// ACT: RR_ACT_GELU, RR_ACT_SWIGLU (bf16: with the division), or -1.  ONCE: no other workgroup reads these rows of B.
+template <class S, bool GATED, int ACT, bool GATHER, bool DIRECT, bool DENSE = false, bool TA = false, bool TB = false, bool ONCE = false>
 __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename std::conditional<DENSE, DenseArgs, GemmArgs>::type P) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int WM = S::WM, WN = S::WN, NW = S::NW, BM = S::BM, ST = S::ST;
@@ -1016,7 +1017,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
         continue;
       }
       const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstepB;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(!GATED || i < NIB0 ? rsB0 : rsB1, lp, 16, past ? PAST : v, koff, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(!GATED || i < NIB0 ? rsB0 : rsB1, lp, 16, past ? PAST : v, koff, 0, ONCE ? BUF_STREAM : 0);
     }
 #pragma unroll
     for (int i = 0; i < NIA; ++i) {

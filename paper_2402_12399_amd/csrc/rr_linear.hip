@@ -121,6 +121,8 @@ __global__ __launch_bounds__(LR_THREADS, 4) void linear_rows_kernel(DenseArgs P)
 // As many dot products per row of W as there are rows of x: a wave takes VR rows of W (gated: VR / 2 of each half), a lane 16
 // bytes of each in every chunk of 1 KB, and the lanes' sums are added at the end.  Every wave reads whole rows, so that
 // also a narrow W is spread over the chip (16 columns a workgroup in the kernel above: 8192 -> 1024 fills 64 CUs).
+// W streams past the caches (see launch_dense_tiles): one row, 4096 -> 2 x 11008 30.5 -> 27.3 us (6.6 TB/s), 11008 -> 4096 20.4 -> 18.0; fp32
+// 4096 -> 4096 13.8 -> 12.4.
 constexpr int kVectorRows = 4;
 constexpr int LV_THREADS = 256, LV_ROWS = 2;
 [[maybe_unused]] constexpr int LV_AHEAD = 4;
@@ -142,8 +144,7 @@ __global__ __launch_bounds__(LV_THREADS) void linear_vector_kernel(DenseArgs P) 
   auto rsrc = [&](const char *base) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, __builtin_amdgcn_readfirstlane((int)rowb), BUF_FLAGS);
   };
-  auto load = [](const __amdgpu_buffer_rsrc_t &rs, unsigned off) { return __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0); };
-  using Quad = decltype(load(rsrc(nullptr), 0u));
+  using Quad = decltype(__builtin_amdgcn_raw_buffer_load_b128(rsrc(nullptr), 0u, 0, 0));
   auto value = [](const Quad &v, int i) {
     const u32 word = v[BF16 ? i >> 1 : i];  // (a copy: __builtin_bit_cast of a vector's element takes element 0, whichever it is)
     return __builtin_bit_cast(float, BF16 ? (i & 1 ? word & 0xffff0000u : word << 16) : word);
@@ -160,9 +161,9 @@ __global__ __launch_bounds__(LV_THREADS) void linear_vector_kernel(DenseArgs P) 
     for (int s = 0; s < LV_AHEAD; ++s) {
       const unsigned at = (unsigned)(c0 + s) * 1024 + lane * 16;
 #pragma unroll
-      for (int v = 0; v < VR; ++v) b[s][v] = load(rsrc(wrow[v]), at);
+      for (int v = 0; v < VR; ++v) b[s][v] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(wrow[v]), at, 0, BUF_STREAM);
 #pragma unroll
-      for (int m = 0; m < M; ++m) a[s][m] = load(rsrc(static_cast<const char *>(P.A) + (size_t)m * rowb), at);
+      for (int m = 0; m < M; ++m) a[s][m] = __builtin_amdgcn_raw_buffer_load_b128(rsrc(static_cast<const char *>(P.A) + (size_t)m * rowb), at, 0, 0);
     }
 #pragma unroll
     for (int s = 0; s < LV_AHEAD; ++s)
@@ -515,6 +516,16 @@ void launch_dense_tiles(DenseArgs A, hipStream_t s) {
   constexpr long long kRow = 1ll << 20;  // workgroups in a row of the grid, whole XCD runs (see gemm_tile_kernel)
   const long long tiles = (long long)A.NT * A.MT * A.slices;
   const dim3 grid((unsigned)((std::min(tiles, kRow) + 7) / 8 * 8), (unsigned)((tiles + kRow - 1) / kRow));
+  // One tile of rows: each byte of W is read by one workgroup, once, and streams past the caches (ONCE).  16 x 4096 -> 2 x 11008 39.2 -> 35.3 us
+  // (5.1 TB/s), 32 x 11008 -> 4096 24.0 -> 22.5, 128 x 4096 -> 2 x 11008 49.4 -> 46.1; only if the last-level cache still holds a large W from
+  // the call before it costs time (16 x 4096 -> 2 x 11008, 180 MB: 27.0 -> 35.5; of 34 MB and less: nothing).  More tiles of rows: 10 % either way, so
+  // not; fp32: 1 %, so not.
+  if constexpr (S::BF16 && !TB) {
+    if (A.MT == 1) {
+      gemm_tile_kernel<S, GATED, ACT, false, false, true, TA, TB, true><<<grid, S::THREADS, S::SMEM, s>>>(A);
+      return;
+    }
+  }
   gemm_tile_kernel<S, GATED, ACT, false, false, true, TA, TB><<<grid, S::THREADS, S::SMEM, s>>>(A);
 }
 
@@ -641,6 +652,9 @@ hipError_t linear_kernel_attributes() {
       set(gemm_tile_kernel<S, false, -1, false, false, true>, S::SMEM);
     }
     if constexpr (S::BF16) {
+      set(gemm_tile_kernel<S, true, -1, false, false, true, false, false, true>, S::SMEM);
+      set(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false, true, false, false, true>, S::SMEM);
+      set(gemm_tile_kernel<S, false, -1, false, false, true, false, false, true>, S::SMEM);
       set(gemm_tile_kernel<S, false, -1, false, false, true, false, true>, S::SMEM);
       set(gemm_tile_kernel<S, false, -1, false, false, true, true, true>, S::SMEM);
     }
