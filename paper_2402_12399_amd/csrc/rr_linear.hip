@@ -78,7 +78,10 @@ __global__ __launch_bounds__(LR_THREADS, 4) void linear_rows_kernel(DenseArgs P)
     }
   };
 #pragma unroll
-  for (int s = 0; s < LR_AHEAD; ++s) fetch(w + s * LR_NW, s);
+  for (int s = 0; s < LR_AHEAD; ++s) {
+    fetch(w + s * LR_NW, s);
+    __builtin_amdgcn_sched_barrier(0);  // in this order, or the loop below waits for all of them at once (16 x 4096 -> 2 x 4096 16.8 us, 15.7 so)
+  }
   for (int c = w; c < chunks; c += LR_AHEAD * LR_NW) {
 #pragma unroll
     for (int s = 0; s < LR_AHEAD; ++s) {
@@ -98,6 +101,7 @@ __global__ __launch_bounds__(LR_THREADS, 4) void linear_rows_kernel(DenseArgs P)
             }
           }
       fetch(c + (LR_AHEAD + s) * LR_NW, s);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
@@ -117,13 +121,15 @@ __global__ __launch_bounds__(LR_THREADS, 4) void linear_rows_kernel(DenseArgs P)
 #endif
 }
 
-// ------------------------------------------------------------------ one to kVectorRows rows
+// ------------------------------------------------------------------ one to four rows
 // As many dot products per row of W as there are rows of x: a wave takes VR rows of W (gated: VR / 2 of each half), a lane 16
 // bytes of each in every chunk of 1 KB, and the lanes' sums are added at the end.  Every wave reads whole rows, so that
-// also a narrow W is spread over the chip (16 columns a workgroup in the kernel above: 8192 -> 1024 fills 64 CUs).
+// also a narrow W is spread over the chip (16 columns a workgroup in the kernel above: 8192 -> 1024 fills 64 CUs).  Each row of W is met by all of
+// x, out of the caches: from 3 rows of bf16 on the other kernels are faster (4 rows, 4096 -> 2 x 11008 41.6 -> 35.4 us, 11008 -> 4096 23.4 -> 18.8;
+// 3 rows 36.3 -> 35.5, 9.1 -> 8.5 for 4096 -> 4096, though 8192 -> 1024 7.6 -> 8.2), from 5 of fp32 (4 rows, 4096 -> 4096 16.1 here, 18.1 there).
 // W streams past the caches (see launch_dense_tiles): one row, 4096 -> 2 x 11008 30.5 -> 27.3 us (6.6 TB/s), 11008 -> 4096 20.4 -> 18.0; fp32
 // 4096 -> 4096 13.8 -> 12.4.
-constexpr int kVectorRows = 4;
+constexpr int kVectorRows(bool bf16) { return bf16 ? 2 : 4; }
 constexpr int LV_THREADS = 256, LV_ROWS = 2;
 [[maybe_unused]] constexpr int LV_AHEAD = 4;
 
@@ -426,20 +432,22 @@ struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_ke
 // Times in us of a dense product's parts: a fit to 970 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 700 fp32
 // ones, each timed in up to 34 pairs of shape and slices.  The plan is 1.2 % (fp32: 1.1 %) off the best pair on average, 1.4 %
 // (1.4 %) on the quarter of them that the fit did not see; the worst of those by 24 % (21 %), most of them products of 4 us.  (The
-// grouped GEMM's numbers, which expect ragged experts and weights from HBM: 7 %, the worst by 45 %.)
-struct DenseShape { float chunk, fixed, alone; };  // as ShapeInfo: of a chunk, of a tile, of a chunk with the CU to itself (split shapes)
+// grouped GEMM's numbers, which expect ragged experts and weights from HBM: 7 %, the worst by 45 %.)  3 .. 32 rows of bf16 with W from HBM,
+// 1744 products in random order: `rows`, `cold`, `alone` and `even` fitted to a third of those, 2.3 % off the best, 3.0 % on the rest.
+struct DenseShape { float chunk, fixed, alone; };  // as ShapeInfo: of a chunk, of a tile, of a chunk with the CU to itself (split shapes; few rows)
 struct DenseTimes {
   int first;             // FfnShape of shape[0]
   DenseShape shape[6];
   float fetch, stream;   // bytes per us that a CU gets of its operands, and all of them together
-  float last, even;      // a last, partial round on top of its share; split shapes: weight of the exact number of rounds
+  float last, even;      // a last, partial round on top of its share; split shapes, few rows: weight of the exact number of rounds
   float launch, join, join_slice, join_bytes;  // of any kernel; of the joining one: itself, per slice, passes over the slices' sums
   float rows;            // linear_rows_kernel: start and end
+  float cold;            // up to kFewRows rows: a chunk's time, W coming from HBM, over that of a product that finds its operands in the caches
 };
-constexpr DenseTimes kBf16Times{FFN_P256, {{1.37f, 0.02f}, {0.787f, 1.05f}, {0.506f, 0.73f}, {0.341f, 0.66f}, {0.273f, 0.73f}, {0.14f, 0.84f}},
-                                153e3f, 10.1e6f, 0.98f, 0.0f, 2.6f, 1.7f, 0.15f, 2.3f, 0.9f};
+constexpr DenseTimes kBf16Times{FFN_P256, {{1.37f, 0.02f}, {0.787f, 1.05f}, {0.506f, 0.73f}, {0.341f, 0.66f, 1.1f}, {0.273f, 0.73f, 0.47f}, {0.14f, 0.84f, 0.19f}},
+                                153e3f, 10.1e6f, 0.98f, 0.5f, 2.6f, 1.7f, 0.15f, 2.3f, 0.8f, 1.39f};
 constexpr DenseTimes kF32Times{FFN_S128, {{1.328f, 0.52f, 1.67f}, {0.738f, 0.24f, 0.99f}, {0.937f, 0.17f}, {0.521f, 0.19f}, {0.26f, 0.02f}, {0.0f, 0.0f}},
-                               38e3f, 91e6f, 0.54f, 0.25f, 3.4f, 2.3f, 0.083f, 1.36f, 0.5f};
+                               38e3f, 91e6f, 0.54f, 0.25f, 3.4f, 2.3f, 0.083f, 1.36f, 0.5f, 1.0f};
 constexpr float kPersistentDense = 3.2f;  // the 256 x 256 kernel's start
 
 // Estimated time of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
@@ -462,9 +470,10 @@ float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, T
   if (slices > 1 && part > kPartBytes) return -1.0f;
   const float stream = (float)((double)(M + R) * K * es + (double)M * N * es) / T.stream;
   const float fetch = (float)GB_ROW_BYTES * ((float)s.brows / mt + (float)s.bm / nt) / T.fetch;
-  const float chunk = std::max(c.chunk, fetch);  // (turned operands: the same, 440 products)
+  const bool few = bf16 && M <= kFewRows && turned == TURNED_NONE;  // W from HBM, read once
+  const float chunk = std::max(c.chunk * (few ? T.cold : 1.0f), fetch);  // (turned operands: the same, 440 products)
   float busy = (float)rounds * (KT * chunk + c.fixed);
-  if (split) {
+  if (split || (few && c.alone > 0.0f)) {
     const float all = (float)tiles / kCUs;
     busy = std::max((T.even * all + (1.0f - T.even) * ceilf(all)) * (KT * chunk + c.fixed), KT * c.alone + c.fixed);
   } else if (persistent) {
@@ -489,7 +498,7 @@ float rows_cost(long long M, long long N, long long K, bool bf16, bool gated) {
 
 DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
   const bool as_is = bf16 && turned != TURNED_NONE;  // tiles only
-  if (M <= kVectorRows && !as_is) return {-1, 1};
+  if (M <= kVectorRows(bf16) && !as_is) return {-1, 1};
   const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : FFN_F32N;
   DensePlan best{q1, 1};
   float least = -1.0f;
@@ -516,8 +525,8 @@ void launch_dense_tiles(DenseArgs A, hipStream_t s) {
   constexpr long long kRow = 1ll << 20;  // workgroups in a row of the grid, whole XCD runs (see gemm_tile_kernel)
   const long long tiles = (long long)A.NT * A.MT * A.slices;
   const dim3 grid((unsigned)((std::min(tiles, kRow) + 7) / 8 * 8), (unsigned)((tiles + kRow - 1) / kRow));
-  // One tile of rows: each byte of W is read by one workgroup, once, and streams past the caches (ONCE).  16 x 4096 -> 2 x 11008 39.2 -> 35.3 us
-  // (5.1 TB/s), 32 x 11008 -> 4096 24.0 -> 22.5, 128 x 4096 -> 2 x 11008 49.4 -> 46.1; only if the last-level cache still holds a large W from
+  // One tile of rows: each byte of W is read by one workgroup, once, and streams past the caches (ONCE).  in the same tiles 16 x 4096 -> 2 x 11008
+  // 39.2 -> 35.3 us (5.1 TB/s), 32 x 11008 -> 4096 24.0 -> 22.5, 128 x 4096 -> 2 x 11008 49.4 -> 46.1; only if the last-level cache still holds a large W from
   // the call before it costs time (16 x 4096 -> 2 x 11008, 180 MB: 27.0 -> 35.5; of 34 MB and less: nothing).  More tiles of rows: 10 % either way, so
   // not; fp32: 1 %, so not.
   if constexpr (S::BF16 && !TB) {
@@ -562,13 +571,13 @@ void launch_product(DenseArgs A, const DensePlan &plan, Turned turned, float *pa
   A.K = plan.slices > 1 ? (A.Kall / plan.slices + ce - 1) / ce * ce : A.Kall;
   A.part = plan.slices > 1 ? part : nullptr;
   if (plan.shape < 0) {
-    if (A.M <= kVectorRows) {
+    if (A.M <= kVectorRows(BF16)) {
       const dim3 grid((A.N * (GATED ? 2 : 1) / LV_ROWS + LV_THREADS / kWave - 1) / (LV_THREADS / kWave));
-      switch (A.M) {
-        case 1: linear_vector_kernel<BF16, GATED, ACT, 1><<<grid, LV_THREADS, 0, s>>>(A); break;
-        case 2: linear_vector_kernel<BF16, GATED, ACT, 2><<<grid, LV_THREADS, 0, s>>>(A); break;
-        case 3: linear_vector_kernel<BF16, GATED, ACT, 3><<<grid, LV_THREADS, 0, s>>>(A); break;
-        default: linear_vector_kernel<BF16, GATED, ACT, 4><<<grid, LV_THREADS, 0, s>>>(A); break;
+      if (A.M == 1) linear_vector_kernel<BF16, GATED, ACT, 1><<<grid, LV_THREADS, 0, s>>>(A);
+      if (A.M == 2) linear_vector_kernel<BF16, GATED, ACT, 2><<<grid, LV_THREADS, 0, s>>>(A);
+      if constexpr (kVectorRows(BF16) > 2) {
+        if (A.M == 3) linear_vector_kernel<BF16, GATED, ACT, 3><<<grid, LV_THREADS, 0, s>>>(A);
+        if (A.M == 4) linear_vector_kernel<BF16, GATED, ACT, 4><<<grid, LV_THREADS, 0, s>>>(A);
       }
       return;
     }

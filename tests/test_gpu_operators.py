@@ -271,7 +271,9 @@ SHAPES = [(1, 8, 8), (2, 24, 16), (1, 4096, 512), (3, 8200, 72), (16, 1000, 264)
 
 # the tiles and slices that the shapes above leave out (test_operators_host.py checks that none is left)
 MORE = [(34, 2712, 4512), (4102, 80, 912), (9095, 8, 1984), (8445, 1688, 8), (1032, 4152, 48), (2471, 5832, 8), (4199, 8, 2864), (5, 5640, 1848),
-        (3650, 8, 2480), (7, 2520, 3008), (1228, 1440, 8)]
+        (3650, 8, 2480), (7, 2520, 3008), (1228, 1440, 8), (26, 480, 4256), (27, 128, 10600), (12, 2800, 5504), (33, 8, 8672), (42, 1592, 8328),
+        (72, 8, 8744), (82, 2952, 5952), (129, 8, 8624), (198, 3224, 10104), (145, 4408, 1224), (38, 2624, 1384), (3, 512, 520), (4, 1000, 264),
+        (31, 512, 264), (3, 5144, 4184), (18, 7920, 9840)]
 
 
 def linear_case(M, K, N, dtype, act, make, seed, bias=True, residual=True):

@@ -299,7 +299,7 @@ def _plan_keys(M, K, N):
         for act in (rr.RR_ACT_NONE, rr.RR_ACT_SWIGLU):
             for role, (bm, brows, slices, parts) in enumerate(gu.linear_plans(rr.RRLinearConfig(M, K, N, dtype, act))):
                 if role == 0 or act == rr.RR_ACT_NONE:
-                    yield dtype, role, bm, brows, parts, slices > 1
+                    yield dtype, role, bm, brows, parts, slices > 1, role == 0 and 0 < bm and M <= bm  # (one tile of rows: weights read once)
 
 
 def test_the_gpu_tests_reach_every_tile(lib):
