@@ -908,7 +908,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "operand boundaries must fall between load instructions");
   static_assert((8 * NW) % 16 == 0, "swizzle must not depend on the instruction index");
   static_assert(!GATED || WN % 2 == 0, "a wave holds the gate and the up columns of its outputs");
-  static_assert(!(TA || TB) || (DENSE && !GATED && !GATHER && S::BF16));
+  static_assert(!(TA || TB) || (DENSE && !GATED && !GATHER && S::MATH != TILE_F32));
   constexpr int kPanel = 8;  // row tiles that share a column tile of weights before the next column tile
   extern __shared__ __attribute__((aligned(16))) char smem[];
 
@@ -986,10 +986,10 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
   // Turned operands: a chunk's rows are a buffer of their own, from the tile's first column on.  Offsets of this lane in instructions
   // 0 and 1 (the swizzle of two instructions apart is the same), bytes between instructions.
   constexpr int TRA = BM * 2, TRB = S::BROWS * 2, RPA = 1024 / TRA, RPB = 1024 / TRB;
-  static_assert(!TA || NW * RPA % 8 == 0);
-  static_assert(!TB || NW * RPB % 8 == 0);
+  static_assert(!TA || !S::BF16 || NW * RPA % 8 == 0);
+  static_assert(!TB || !S::BF16 || NW * RPB % 8 == 0);
   unsigned ta[2] = {0, 0}, tb[2] = {0, 0};
-  if constexpr (TA || TB) {
+  if constexpr ((TA || TB) && S::BF16) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       int row, byte;
@@ -1044,7 +1044,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     b_off[j] = (BM + row) * GB_ROW_BYTES;
   }
   int a_turn[WM], b_turn[WN];
-  if constexpr (TA || TB) {
+  if constexpr ((TA || TB) && S::BF16) {
 #pragma unroll
     for (int i = 0; i < WM; ++i) a_turn[i] = turned_at<TRA>(wm * WM + i, fr, fg);
 #pragma unroll
@@ -1061,12 +1061,12 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     const int pos = ((4 * ks + fg) ^ fsw) << 4;
 #pragma unroll
     for (int i = 0; i < WM; ++i) {
-      if constexpr (TA) af[ks][i] = read_turned<TRA>(st + a_turn[i] + ks * 32 * TRA);
+      if constexpr (TA && S::BF16) af[ks][i] = read_turned<TRA>(st + a_turn[i] + ks * 32 * TRA);
       else af[ks][i] = *reinterpret_cast<const Frag *>(st + a_off[i] + pos);
     }
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
-      if constexpr (TB) bfr[ks][j] = read_turned<TRB>(st + b_turn[j] + ks * 32 * TRB);
+      if constexpr (TB && S::BF16) bfr[ks][j] = read_turned<TRB>(st + b_turn[j] + ks * 32 * TRB);
       else bfr[ks][j] = *reinterpret_cast<const Frag *>(st + b_off[j] + pos);
     }
   };
@@ -1104,31 +1104,73 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     // Chunks go through registers: a lane holds four elements of NI rows, splits them and writes 8 bytes to each of the
     // three planes in LDS, 64 bytes per row and chunk; the next chunk is requested before this one is multiplied.
     f32x4 raw[NI];
-    auto fetch = [&](int kt) {
-      const bool past = kt * CE + piece * PE >= K;
-      const int koff = min(kt, KT - 1) * GB_ROW_BYTES;
-#pragma unroll
-      for (int i = 0; i < NIB; ++i) {
-        const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstepB;
-        raw[NIA + i] = load16(!GATED || i < NIB0 ? rsB0 : rsB1, past ? PAST : v, koff);
-      }
-#pragma unroll
-      for (int i = 0; i < NIA; ++i) {
-        const unsigned v = GATHER ? va[GATHER ? i : 0] : va[0] + i * rstep;
-        raw[i] = load16(rsA, past ? PAST : v, koff);
-      }
-    };
     // 16-byte piece c of a plane's row sits at c ^ ((row >> 2) & 3): the 16 rows of a fragment then fill all 64 banks
     constexpr int PLANE = (BM + S::BROWS) * GB_ROW_BYTES / 2;
     char *const wr = smem + lrow * 64 + (((piece >> 1) ^ ((lrow >> 2) & 3)) << 4) + (piece & 1) * 8;
     const int fpos = fr * 64 + ((fg ^ (fr >> 2)) << 4);
+    // A turned operand (row k of the chunk holds the elements k of all rows): a lane reads four rows' elements of as many k as
+    // it has instructions, a block that it turns by taking the registers the other way round.  Row r of such a plane sits at
+    // (r & 3) * rows / 4 + (r >> 2), its piece c at c ^ (r & 3): a wave's writes, eight neighbours of a quarter, and a
+    // fragment's reads both fill all banks.
+    const int tca = (TA && NIA == 2 ? w & 1 : w) * 8 + (lane & 7), tka = (lane >> 3) + (TA && NIA == 2 ? (w >> 1) * 8 : 0);  // block: 4 rows; NIA k
+    const int tcb = w * 8 + (lane & 7), tkb = lane >> 3;
+    static_assert(!(TA || TB) || (NW == 4 && !GATED && !GATHER));
+    static_assert(!TA || (NIA == 4 && BM == 128) || (NIA == 2 && BM == 64));
+    static_assert(!TB || (NIB == 4 && S::BROWS == 128));
+    auto fetch_turned = [&](f32x4 *r, int n, const __amdgpu_buffer_rsrc_t &rs, int k, int c, unsigned pitch) {
+#pragma unroll
+      for (int i = 0; i < n; ++i) r[i] = load16(rs, (k * n + i) * pitch + c * 16, 0);
+    };
+    auto write_turned = [&](const f32x4 *r, int n, char *region, int rows, int k, int c, float scale) {
+#pragma unroll
+      for (int j = 0; j < 4; j += n == 4 ? 1 : 2) {
+        uint2 q[3];
+        split3(n == 4 ? f32x4{r[0][j], r[1][j], r[n - 2][j], r[n - 1][j]} : f32x4{r[0][j], r[1][j], r[0][(j + 1) & 3], r[1][(j + 1) & 3]}, scale, q);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          char *at = region + p * PLANE + (j * (rows / 4) + c) * 64;
+          if (n == 4) {
+            *reinterpret_cast<uint2 *>(at + (((k >> 1) ^ j) << 4) + (k & 1) * 8) = q[p];
+          } else {
+            *reinterpret_cast<u32 *>(at + (((k >> 2) ^ j) << 4) + (k & 3) * 4) = q[p].x;
+            *reinterpret_cast<u32 *>(at + rows / 4 * 64 + (((k >> 2) ^ (j + 1)) << 4) + (k & 3) * 4) = q[p].y;
+          }
+        }
+        if (WM == 4 && j % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    const int tpos = (fr >> 2) * 64 + ((fg ^ (fr & 3)) << 4);
+    auto fetch = [&](int kt) {
+      const bool past = kt * CE + piece * PE >= K;
+      const int koff = min(kt, KT - 1) * GB_ROW_BYTES;
+      if constexpr (TB) {
+        fetch_turned(raw + NIA, NIB, turned_rsrc(P.B0, kt, rowbB, n0), tkb, tcb, rowbB);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NIB; ++i) {
+          const unsigned v = vb + (GATED && i >= NIB0 ? i - NIB0 : i) * rstepB;
+          raw[NIA + i] = load16(!GATED || i < NIB0 ? rsB0 : rsB1, past ? PAST : v, koff);
+        }
+      }
+      if constexpr (TA) {
+        fetch_turned(raw, NIA, turned_rsrc(P.A, kt, rowb, m0), tka, tca, rowb);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NIA; ++i) {
+          const unsigned v = GATHER ? va[GATHER ? i : 0] : va[0] + i * rstep;
+          raw[i] = load16(rsA, past ? PAST : v, koff);
+        }
+      }
+    };
     float scale;  // in a register: a multiplication of 4 bytes instead of 8
     asm("s_mov_b32 %0, %1" : "=s"(scale) : "i"(__builtin_bit_cast(int, kSplitScale)));
     fetch(0);
     for (int kt = 0; kt < KT; ++kt) {
       if (kt > 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // everybody has read chunk kt - 1
+      if constexpr (TA) write_turned(raw, NIA, smem, BM, tka, tca, scale);
+      if constexpr (TB) write_turned(raw + NIA, NIB, smem + BM * 64, S::BROWS, tkb, tcb, scale);
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
+      for (int i = TA ? NIA : 0; i < (TB ? NIA : NI); ++i) {
         uint2 q[3];
         split3(raw[i], scale, q);
 #pragma unroll
@@ -1144,13 +1186,15 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
       for (int j = 0; j < WN; ++j)
 #pragma unroll
         for (int p = 0; p < 3; ++p)
-          b3[j][p] = *reinterpret_cast<const bf16x8 *>(smem + p * PLANE + (b_off[j] / GB_ROW_BYTES - fr) * 64 + fpos);
+          b3[j][p] = *reinterpret_cast<const bf16x8 *>(smem + p * PLANE + (TB ? (BM + (fr & 3) * (S::BROWS / 4) + (wn * WN + j) * 4) * 64 + tpos
+                                                                              : (b_off[j] / GB_ROW_BYTES - fr) * 64 + fpos));
 #pragma unroll
       for (int i = 0; i < WM; ++i) {
         bf16x8 a3[3];
 #pragma unroll
         for (int p = 0; p < 3; ++p)
-          a3[p] = *reinterpret_cast<const bf16x8 *>(smem + p * PLANE + (wm * WM + i) * 16 * 64 + fpos);
+          a3[p] = *reinterpret_cast<const bf16x8 *>(smem + p * PLANE + (TA ? ((fr & 3) * (BM / 4) + (wm * WM + i) * 4) * 64 + tpos
+                                                                           : (wm * WM + i) * 16 * 64 + fpos));
         // the products of parts down to 2^-18 of the leading one, smallest first
         constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};
 #pragma unroll
@@ -1160,6 +1204,13 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b3[j][PB[q]], a3[PA[q]], acc[i][j], 0, 0, 0);
       }
     }
+    auto four_of_turned = [&](const void *base, unsigned pitch, int k, int row, int rows) {
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (k + u < K && row < rows) v[u] = *reinterpret_cast<const float *>(static_cast<const char *>(base) + (size_t)(k0 + k + u) * pitch + (size_t)row * 4);
+      return v;
+    };
     // An infinity, or a value that the scale or bf16's rounding makes one, leaves NaN behind its first part: a fragment of
     // which any element is not finite is computed again from fp32 operands.
 #pragma unroll
@@ -1183,7 +1234,11 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
         for (int k = 0; k < K; k += 16) {
           const unsigned kb = (k + 4 * fg) * ES;
           const bool past = kb >= (unsigned)K * ES;
-          const f32x4 a = load16(rsA, past || ao == PAST ? PAST : ao + kb, 0), b = load16(up ? rsB1 : rsB0, past ? PAST : bo + kb, 0);
+          f32x4 a, b;
+          if constexpr (TA) a = four_of_turned(P.A, rowb, k + 4 * fg, m0 + arow, rows_e);
+          else a = load16(rsA, past || ao == PAST ? PAST : ao + kb, 0);
+          if constexpr (TB) b = four_of_turned(P.B0, rowbB, k + 4 * fg, n0 + (wn * WN + j) * 16 + fr, N);
+          else b = load16(up ? rsB1 : rsB0, past ? PAST : bo + kb, 0);
 #pragma unroll
           for (int u = 0; u < 4; ++u) c = __builtin_amdgcn_mfma_f32_16x16x4f32(b[u], a[u], c, 0, 0, 0);
         }

@@ -517,6 +517,23 @@ DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gate
   return best;
 }
 
+// The gradients' products: whether the operands are read as they lie.
+struct TurnedPlan {
+  DensePlan plan;
+  bool as_is;
+};
+bool splits(const DensePlan &p) { return p.shape == FFN_S128 || p.shape == FFN_S64; }
+TurnedPlan plan_dx(const rr_linear_config &c, int R, bool bf16) {
+  const DensePlan p = dense_plan(c.M, c.K, R, bf16, false, TURNED_B);
+  return {p, bf16 || splits(p)};
+}
+// LT: length of the transposes' rows, where they are made
+TurnedPlan plan_dw(const rr_linear_config &c, int R, bool bf16, int LT) {
+  const DensePlan p = dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH);
+  if (bf16 || splits(p)) return {p, true};
+  return {dense_plan(R, c.K, LT, bf16, false, TURNED_BOTH), false};
+}
+
 template <class S, bool GATED, int ACT, bool TA, bool TB>
 void launch_dense_tiles(DenseArgs A, hipStream_t s) {
   constexpr int bn = GATED ? S::BROWS / 2 : S::BROWS;
@@ -557,8 +574,12 @@ void launch_dense_shape(int shape, DenseArgs A, hipStream_t s) {
     switch (shape) {
       case FFN_S128: launch_dense_tiles<TileS128, GATED, ACT, TA, TB>(A, s); break;
       case FFN_S64: launch_dense_tiles<TileS64, GATED, ACT, TA, TB>(A, s); break;
-      case FFN_F64: launch_dense_tiles<TileF64, GATED, ACT, TA, TB>(A, s); break;
-      default: launch_dense_tiles<TileF32n, GATED, ACT, TA, TB>(A, s); break;
+      case FFN_F64:
+        if constexpr (!TB) launch_dense_tiles<TileF64, GATED, ACT, TA, TB>(A, s);
+        break;
+      default:
+        if constexpr (!TB) launch_dense_tiles<TileF32n, GATED, ACT, TA, TB>(A, s);
+        break;
     }
   }
 }
@@ -586,7 +607,7 @@ void launch_product(DenseArgs A, const DensePlan &plan, Turned turned, float *pa
     else linear_rows_kernel<BF16, GATED, ACT, 2><<<grid, LR_THREADS, 0, s>>>(A);
     return;
   }
-  if constexpr (BF16 && !GATED && ACT < 0) {
+  if constexpr (!GATED && ACT < 0) {
     if (turned == TURNED_B) launch_dense_shape<BF16, GATED, ACT, false, true>(plan.shape, A, s);
     if (turned == TURNED_BOTH) launch_dense_shape<BF16, GATED, ACT, true, true>(plan.shape, A, s);
   }
@@ -664,6 +685,8 @@ hipError_t linear_kernel_attributes() {
       set(gemm_tile_kernel<S, true, -1, false, false, true, false, false, true>, S::SMEM);
       set(gemm_tile_kernel<S, false, RR_ACT_GELU, false, false, true, false, false, true>, S::SMEM);
       set(gemm_tile_kernel<S, false, -1, false, false, true, false, false, true>, S::SMEM);
+    }
+    if constexpr (S::MATH != TILE_F32) {
       set(gemm_tile_kernel<S, false, -1, false, false, true, false, true>, S::SMEM);
       set(gemm_tile_kernel<S, false, -1, false, false, true, true, true>, S::SMEM);
     }
@@ -681,8 +704,7 @@ void linear_describe(const rr_linear_config &c, LinearPlans *out) {
   const bool bf16 = c.dtype == RR_BF16;
   const int R = width(c);
   const DensePlan plan[3] = {dense_plan(c.M, c.N, c.K, bf16, c.act == RR_ACT_SWIGLU, TURNED_NONE),
-                             dense_plan(c.M, c.K, R, bf16, false, TURNED_B),
-                             dense_plan(R, c.K, bf16 ? c.M : backward_work(c, nullptr).LT, bf16, false, TURNED_BOTH)};
+                             plan_dx(c, R, bf16).plan, plan_dw(c, R, bf16, backward_work(c, nullptr).LT).plan};
   for (int i = 0; i < 3; ++i) {
     out->bm[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].bm;
     out->brows[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].brows;
@@ -738,22 +760,24 @@ hipError_t launch_linear_backward(const rr_linear_config &c, const void *x, cons
     else launch_product<false, false, -1>(A, plan, turned, W.part, s);
   };
   const bool act = c.act != RR_ACT_NONE;
-  const DensePlan plan_x = dense_plan(c.M, c.K, R, bf16, false, TURNED_B), plan_w = dense_plan(R, c.K, bf16 ? c.M : W.LT, bf16, false, TURNED_BOTH);
-  const TurnArgs make{dy, pre, act && (dx || (dw && bf16)) ? W.dz : nullptr, dw && !bf16 ? W.dz_turned : nullptr,
+  const TurnedPlan px = plan_dx(c, R, bf16), pw = plan_dw(c, R, bf16, W.LT);
+  const TurnArgs make{dy, pre, act && (dx || (dw && pw.as_is)) ? W.dz : nullptr, dw && !pw.as_is ? W.dz_turned : nullptr,
                       dbias ? W.sums : nullptr, c.M, c.N, W.LT};
   const void *dz = act ? W.dz : dy;
   prof_begin(K_LINEAR_BWD, s);
   if (make.dz || make.turned || make.sums) turn(c.act, make);
   if (dbias) linear_bias_kernel<<<(R + kWave - 1) / kWave, LB_PARTS * kWave, 0, s>>>(W.sums, turn_blocks(make), R, dbias);
-  if (dx) {
-    if (!bf16) turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
-    if (bf16) product(dz, R, w, c.K, dx, c.M, c.K, R, plan_x, TURNED_B);
-    else product(dz, R, W.w_turned, R, dx, c.M, c.K, R, plan_x, TURNED_NONE);
+  if (dx && px.as_is) {
+    product(dz, R, w, c.K, dx, c.M, c.K, R, px.plan, TURNED_B);
+  } else if (dx) {
+    turn(RR_ACT_NONE, TurnArgs{w, nullptr, nullptr, W.w_turned, nullptr, R, c.K, R});
+    product(dz, R, W.w_turned, R, dx, c.M, c.K, R, px.plan, TURNED_NONE);
   }
-  if (dw) {
-    if (!bf16) turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
-    if (bf16) product(dz, R, x, c.K, dw, R, c.K, c.M, plan_w, TURNED_BOTH);
-    else product(W.dz_turned, W.LT, W.x_turned, W.LT, dw, R, c.K, W.LT, plan_w, TURNED_NONE);
+  if (dw && pw.as_is) {
+    product(dz, R, x, c.K, dw, R, c.K, c.M, pw.plan, TURNED_BOTH);
+  } else if (dw) {
+    turn(RR_ACT_NONE, TurnArgs{x, nullptr, nullptr, W.x_turned, nullptr, c.M, c.K, W.LT});
+    product(W.dz_turned, W.LT, W.x_turned, W.LT, dw, R, c.K, W.LT, pw.plan, TURNED_NONE);
   }
   prof_end(K_LINEAR_BWD, s);
   return hipGetLastError();
