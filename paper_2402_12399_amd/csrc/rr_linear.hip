@@ -2,8 +2,8 @@
 //
 // Every product is "A[rows, K] times B[N, K]^T" with K contiguous in both operands (rr_gemm.h):
 //   forward  x, W                 dx  dz, W^T                 dw  dz^T, x^T
-// bf16 tiles read the operands of the gradients as they lie in memory ("turned" operands); for fp32 ones linear_turn_kernel
-// writes the transposes.  It also makes dz from dy and the stored z, and sums its columns.
+// bf16 tiles, and fp32 tiles that split their operands, read those of the gradients as they lie in memory ("turned" operands); for
+// other fp32 kernels linear_turn_kernel writes the transposes.  It also makes dz from dy and the stored z, and sums its columns.
 // Which kernel multiplies is a matter of estimated time (dense_plan): 256 x 256 tiles of the persistent kernel, smaller
 // tiles, either with the summation cut into slices where the tiles alone would leave CUs idle (each slice's raw sums go
 // to the workspace and linear_join_kernel adds them in order and does the epilogue), or, up to kFewRows rows,
@@ -427,7 +427,11 @@ size_t part_bytes(size_t M, size_t R, int slices) { return M * R * 4 * slices; }
 // the workspace for them: of a product of M rows it also serves every product of fewer rows
 size_t part_reserve(size_t M, size_t R) { return up256(std::min(part_bytes(M, R, kMaxSlices), kPartBytes)); }
 
-struct DensePlan { int shape, slices; };  // shape: FfnShape; -1: linear_rows_kernel
+struct DensePlan {
+  int shape, slices;  // shape: FfnShape; -1: linear_rows_kernel
+  float time;         // estimate, us
+};
+bool splits(const DensePlan &p) { return p.shape == FFN_S128 || p.shape == FFN_S64; }
 
 // Times in us of a dense product's parts: a fit to 970 bf16 products (M 5 .. 16384, rows and columns 64 .. 11008) and 700 fp32
 // ones, each timed in up to 34 pairs of shape and slices.  The plan is 1.2 % (fp32: 1.1 %) off the best pair on average, 1.4 %
@@ -451,7 +455,7 @@ constexpr DenseTimes kF32Times{FFN_S128, {{1.328f, 0.52f, 1.67f}, {0.738f, 0.24f
 constexpr float kPersistentDense = 3.2f;  // the 256 x 256 kernel's start
 
 // Estimated time of A[M, K] times B[N, K]^T (gated: of two such) in tiles of shape q with K cut into `slices`; < 0: not possible.
-// turned: B, or both operands, lie the other way round (fp32: after the transposes, which every plan needs, they do not).
+// turned: B, or both operands, lie the other way round (fp32: the price of transposes is gradient_plan's).
 enum Turned { TURNED_NONE, TURNED_B, TURNED_BOTH };
 float dense_cost(long long M, long long N, long long K, bool bf16, bool gated, Turned turned, int q, int slices) {
   constexpr int kCUs = 256;
@@ -496,22 +500,19 @@ float rows_cost(long long M, long long N, long long K, bool bf16, bool gated) {
   return T.launch + T.rows + (float)((blocks + 255) / 256) * (float)bytes / (blocks > 256 ? kShared : kAlone);
 }
 
-DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated, Turned turned) {
-  const bool as_is = bf16 && turned != TURNED_NONE;  // tiles only
-  if (M <= kVectorRows(bf16) && !as_is) return {-1, 1};
-  const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : FFN_F32N;
-  DensePlan best{q1, 1};
-  float least = -1.0f;
-  if (M <= kFewRows && !as_is) {
-    best = {-1, 1};
-    least = rows_cost(M, N, K, bf16, gated);
-  }
+// splits_only: of the shapes that split fp32 operands (time < 0: none can)
+DensePlan dense_plan(long long M, long long N, long long K, bool bf16, bool gated, Turned turned, bool splits_only = false) {
+  const bool tiles_only = splits_only || (bf16 && turned != TURNED_NONE);
+  if (M <= kVectorRows(bf16) && !tiles_only) return {-1, 1, rows_cost(M, N, K, bf16, gated)};
+  const int q0 = bf16 ? FFN_P256 : FFN_S128, q1 = bf16 ? FFN_32N : splits_only ? FFN_S64 : FFN_F32N;
+  DensePlan best{q1, 1, -1.0f};
+  if (M <= kFewRows && !tiles_only) best = {-1, 1, rows_cost(M, N, K, bf16, gated)};
   for (int q = q0; q <= q1; ++q) {
     if (q == FFN_F32) continue;  // (32 x 128 in fp32: the best estimate of one product in 5000, by nothing)
     const long long bn = gated ? kShape[q].brows / 2 : kShape[q].brows, tiles = (M + kShape[q].bm - 1) / kShape[q].bm * ((N + bn - 1) / bn);
     for (int s = 1; s <= kMaxSlices && (s == 1 || tiles * s <= 2048); ++s) {  // (eight rounds: slices even nothing out any more)
       const float t = dense_cost(M, N, K, bf16, gated, turned, q, s);
-      if (t >= 0.0f && (least < 0.0f || t < least)) { least = t; best = {q, s}; }
+      if (t >= 0.0f && (best.time < 0.0f || t < best.time)) best = {q, s, t};
     }
   }
   return best;
@@ -522,16 +523,22 @@ struct TurnedPlan {
   DensePlan plan;
   bool as_is;
 };
-bool splits(const DensePlan &p) { return p.shape == FFN_S128 || p.shape == FFN_S64; }
+// fp32: tiles that split their operands turn them too; of other kernels the transposes before them are a part of the price (16 x
+// 4096 -> 4096: 74 us with a transpose of W for linear_rows_kernel, 58 in tiles of 64 rows; 818 x 5848 -> 88: 46, 42).
+// `turned`: bytes that those read and write.
+TurnedPlan gradient_plan(const DensePlan &as_is, const DensePlan &any, size_t turned) {
+  if (as_is.time >= 0.0f && as_is.time <= any.time + kF32Times.launch + (float)turned / kHbm) return {as_is, true};
+  return {any, false};
+}
 TurnedPlan plan_dx(const rr_linear_config &c, int R, bool bf16) {
-  const DensePlan p = dense_plan(c.M, c.K, R, bf16, false, TURNED_B);
-  return {p, bf16 || splits(p)};
+  if (bf16) return {dense_plan(c.M, c.K, R, bf16, false, TURNED_B), true};
+  return gradient_plan(dense_plan(c.M, c.K, R, bf16, false, TURNED_B, true), dense_plan(c.M, c.K, R, bf16, false, TURNED_B), (size_t)R * c.K * 8);
 }
 // LT: length of the transposes' rows, where they are made
 TurnedPlan plan_dw(const rr_linear_config &c, int R, bool bf16, int LT) {
-  const DensePlan p = dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH);
-  if (bf16 || splits(p)) return {p, true};
-  return {dense_plan(R, c.K, LT, bf16, false, TURNED_BOTH), false};
+  if (bf16) return {dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH), true};
+  return gradient_plan(dense_plan(R, c.K, c.M, bf16, false, TURNED_BOTH, true), dense_plan(R, c.K, LT, bf16, false, TURNED_BOTH),
+                       (size_t)LT * (2 * c.K + R) * 4);
 }
 
 template <class S, bool GATED, int ACT, bool TA, bool TB>

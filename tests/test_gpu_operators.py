@@ -499,6 +499,17 @@ def test_linear_f32_keeps_the_whole_range(M, K, N, ex, ew):
     assert torch.equal(y.double(), want)
 
 
+@pytest.mark.parametrize("M,K,N", [(37, 520, 264), (130, 264, 1032), (1030, 2048, 1544), (700, 1000, 200)])
+@pytest.mark.parametrize("ed,eo", [(60, 40), (-100, -20), (-140, 20), (20, -60)])
+def test_gradients_f32_keep_the_whole_range(M, K, N, ed, eo):
+    """As above, of operands that lie the other way round."""
+    x, w, _, _, _ = linear_case(M, K, N, "f32", "none", whole, 21, False, False)
+    dy = whole(gen(22), M, N, dtype=F32)
+    got = run_backward(x * 2.0 ** eo, w * 2.0 ** eo, None, dy * 2.0 ** ed, "none", "f32", N, ("dx", "dw"))
+    for name, want in (("dx", torch.mm(dy.double(), w.double())), ("dw", torch.mm(dy.double().t().contiguous(), x.double()))):
+        assert torch.equal(got[name].double(), want * 2.0 ** (ed + eo)), name
+
+
 def test_linear_bias_needs_four_byte_alignment_only():
     for M, act in ((2, "none"), (40, "gelu"), (300, "swiglu")):
         x, w, b, r, R = linear_case(M, 264, 136, "bf16", act, normal, 10)
