@@ -1118,22 +1118,28 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     static_assert(!TA || (NIA == 4 && BM == 128) || (NIA == 2 && BM == 64));
     static_assert(!TB || (NIB == 4 && S::BROWS == 128));
     auto fetch_turned = [&](f32x4 *r, int n, const __amdgpu_buffer_rsrc_t &rs, int k, int c, unsigned pitch) {
+      unsigned at = k * n * pitch + c * 16;
+      // Tiles of 64 rows add up the other offsets again for every chunk: kept in registers, they make others spill (20000 x 512 -> 512
+      // 169 us, 159 so; 128 x 128 tiles lose 2 % by it)
+      if (WM == 2) asm volatile("" : "+v"(at));
 #pragma unroll
-      for (int i = 0; i < n; ++i) r[i] = load16(rs, (k * n + i) * pitch + c * 16, 0);
+      for (int i = 0; i < n; ++i) r[i] = load16(rs, at + i * pitch, 0);
     };
-    auto write_turned = [&](const f32x4 *r, int n, char *region, int rows, int k, int c, float scale) {
+    auto write_turned = [&](const f32x4 *r, int n, int region, int rows, int k, int c, float scale) {
+      int base = c * 64 + (n == 4 ? ((k >> 1) << 4) + (k & 1) * 8 : ((k >> 2) << 4) + (k & 3) * 4);
+      if (WM == 2) asm volatile("" : "+v"(base));  // likewise
 #pragma unroll
       for (int j = 0; j < 4; j += n == 4 ? 1 : 2) {
         uint2 q[3];
         split3(n == 4 ? f32x4{r[0][j], r[1][j], r[n - 2][j], r[n - 1][j]} : f32x4{r[0][j], r[1][j], r[0][(j + 1) & 3], r[1][(j + 1) & 3]}, scale, q);
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
-          char *at = region + p * PLANE + (j * (rows / 4) + c) * 64;
+          const int at = region + p * PLANE + j * (rows / 4) * 64;
           if (n == 4) {
-            *reinterpret_cast<uint2 *>(at + (((k >> 1) ^ j) << 4) + (k & 1) * 8) = q[p];
+            *reinterpret_cast<uint2 *>(smem + (base ^ (j << 4)) + at) = q[p];
           } else {
-            *reinterpret_cast<u32 *>(at + (((k >> 2) ^ j) << 4) + (k & 3) * 4) = q[p].x;
-            *reinterpret_cast<u32 *>(at + rows / 4 * 64 + (((k >> 2) ^ (j + 1)) << 4) + (k & 3) * 4) = q[p].y;
+            *reinterpret_cast<u32 *>(smem + (base ^ (j << 4)) + at) = q[p].x;
+            *reinterpret_cast<u32 *>(smem + (base ^ ((j + 1) << 4)) + at + rows / 4 * 64) = q[p].y;
           }
         }
         if (WM == 4 && j % 2 == 1) __builtin_amdgcn_sched_barrier(0);
@@ -1167,8 +1173,8 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     fetch(0);
     for (int kt = 0; kt < KT; ++kt) {
       if (kt > 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // everybody has read chunk kt - 1
-      if constexpr (TA) write_turned(raw, NIA, smem, BM, tka, tca, scale);
-      if constexpr (TB) write_turned(raw + NIA, NIB, smem + BM * 64, S::BROWS, tkb, tcb, scale);
+      if constexpr (TA) write_turned(raw, NIA, 0, BM, tka, tca, scale);
+      if constexpr (TB) write_turned(raw + NIA, NIB, BM * 64, S::BROWS, tkb, tcb, scale);
 #pragma unroll
       for (int i = TA ? NIA : 0; i < (TB ? NIA : NI); ++i) {
         uint2 q[3];
