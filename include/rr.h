@@ -216,8 +216,9 @@ int rr_router_backward(const rr_config *cfg, const void *dout, const float *logi
  *   counts      [E+1] int32 out: c_e, then n
  *   mean_prob   [E] fp32 out or NULL: P_e; 0 if no token counts
  *   workspace   rr_balance_workspace_bytes(cfg); not the layer's own, which rr_router_backward still reads
- * logits, rank_expert, loss, counts and mean_prob 4-byte aligned.  Of cfg T, E and k are used.  Sums over tokens are held in 64
- * bits and added in a fixed order: results do not change from run to run. */
+ * logits, rank_expert, loss, counts and mean_prob 4-byte aligned.  Outputs overlap neither each other nor an input
+ * (RR_ERR_INVALID_ARG).  Of cfg T, E and k are used.  Sums over tokens are held in 64 bits and added in a fixed order: results do not
+ * change from run to run. */
 int rr_balance_workspace_bytes(const rr_config *cfg, size_t *bytes);
 int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *rank_expert, const uint8_t *token_mask,
                     float coef, float *loss, int32_t *counts, float *mean_prob,
@@ -229,7 +230,7 @@ int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *ra
  *   dloss       [1] fp32 on the device, or NULL for 1
  *   grad_flags  0, or RR_GRAD_ACCUMULATE: added to what dlogits holds (rr_router_backward's, say); rows of tokens that do not
  *               count are then left as they are
- *   dlogits     [T,E] fp32 in/out; shares no memory with logits (RR_ERR_INVALID_ARG) */
+ *   dlogits     [T,E] fp32 in/out; shares no memory with an input (RR_ERR_INVALID_ARG) */
 #define RR_GRAD_ACCUMULATE 2u
 int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const int32_t *counts, const uint8_t *token_mask,
                              float coef, const float *dloss, uint32_t grad_flags, float *dlogits, void *stream);

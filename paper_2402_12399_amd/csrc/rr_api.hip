@@ -423,6 +423,9 @@ int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *ra
   if (!aligned4(logits) || !aligned4(rank_expert) || !aligned4(loss) || !aligned4(counts) || !aligned4(mean_prob))
     return RR_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < balance_workspace()) return RR_ERR_WORKSPACE;
+  const size_t T = D.T, E = D.E;
+  if (any_meet({{loss, 4}, {counts, (E + 1) * 4}, {mean_prob, E * 4}}, {{logits, T * E * 4}, {rank_expert, T * (D.k + 1) * 4}, {token_mask, T}}))
+    return RR_ERR_INVALID_ARG;
   const hipError_t e = launch_balance_loss(D.T, D.E, D.k, logits, rank_expert, token_mask, coef, loss, counts, mean_prob, workspace,
                                            static_cast<hipStream_t>(stream));
   return e == hipSuccess ? RR_OK : RR_ERR_HIP;
@@ -433,10 +436,11 @@ int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const in
   Dims D;
   const int rc = make_dims(cfg, false, &D);
   if (rc != RR_OK) return rc;
-  const size_t scores = (size_t)D.T * D.E * 4;
-  if (!logits || !counts || !dlogits || meet({logits, scores}, {dlogits, scores}) || !isfinite(coef)) return RR_ERR_INVALID_ARG;
+  if (!logits || !counts || !dlogits || !isfinite(coef)) return RR_ERR_INVALID_ARG;
   if (grad_flags & ~(uint32_t)RR_GRAD_ACCUMULATE) return RR_ERR_INVALID_ARG;
   if (!aligned4(logits) || !aligned4(counts) || !aligned4(dloss) || !aligned4(dlogits)) return RR_ERR_INVALID_ARG;
+  const size_t T = D.T, E = D.E;
+  if (any_meet({{dlogits, T * E * 4}}, {{logits, T * E * 4}, {counts, (E + 1) * 4}, {token_mask, T}, {dloss, 4}})) return RR_ERR_INVALID_ARG;
   const hipError_t e = launch_balance_grad(D.T, D.E, D.k, logits, counts, token_mask, coef, dloss,
                                            (grad_flags & RR_GRAD_ACCUMULATE) != 0, dlogits, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? RR_OK : RR_ERR_HIP;

@@ -197,6 +197,34 @@ def test_dropout_and_balance_outputs_do_not_overlap(lib):
         assert lib.rr_balance_loss_backward(C.byref(c), at(gap), at(5 * gap), None, 0.1, None, 2, at(gap + place), None) == INVALID
 
 
+def test_balance_outputs_do_not_overlap(lib):
+    """Each pair that may not meet, by as little as four bytes (the mask: one); counts are read while dlogits is written."""
+    T, E, k = 64, 8, 2
+    c = rr.RRConfig(T=T, d_model=64, d_ff=0, E=E, k=k, G=2, capacity_factor=1.0).c()
+    gap = 1 << 15
+    size = dict(logits=4 * T * E, rank=4 * T * (k + 1), mask=T, loss=4, counts=4 * (E + 1), mean=4 * E)
+    good = {name: gap * i for i, name in enumerate(size)}
+
+    def forward(**kw):
+        a = {name: at(v) for name, v in dict(good, **kw).items()}
+        return lib.rr_balance_loss(C.byref(c), a["logits"], a["rank"], a["mask"], 0.1, a["loss"], a["counts"], a["mean"], at(8 * gap), BIG, None)
+    for out in ("loss", "counts", "mean"):
+        for other in size:
+            if other != out:
+                for place in (good[other] - size[out] + 4, good[other], good[other] + size[other] - 4):
+                    assert forward(**{out: place}) == INVALID, (out, other, place)
+    size = dict(logits=4 * T * E, counts=4 * (E + 1), mask=T, dloss=4, dlogits=4 * T * E)
+    good = {name: gap * i for i, name in enumerate(size)}
+
+    def backward(flags, **kw):
+        a = {name: at(v) for name, v in dict(good, **kw).items()}
+        return lib.rr_balance_loss_backward(C.byref(c), a["logits"], a["counts"], a["mask"], 0.1, a["dloss"], flags, a["dlogits"], None)
+    for other in ("logits", "counts", "mask", "dloss"):
+        for place in (good[other] - size["dlogits"] + 4, good[other], good[other] + size[other] - 4):
+            for flags in (0, 2):
+                assert backward(flags, dlogits=place) == INVALID, (other, place)
+
+
 def test_dropout_refusals(lib):
     def call(n=64, dtype=rr.RR_BF16, x=FAKE, residual=None, p=0.1, dev=None, out=FAKE):
         a = lib.rr_dropout(n, dtype, x, residual, p, 1, 2, dev, out, None)
