@@ -216,8 +216,8 @@ int rr_router_backward(const rr_config *cfg, const void *dout, const float *logi
  *   counts      [E+1] int32 out: c_e, then n
  *   mean_prob   [E] fp32 out or NULL: P_e; 0 if no token counts
  *   workspace   rr_balance_workspace_bytes(cfg); not the layer's own, which rr_router_backward still reads
- * logits, rank_expert, loss, counts and mean_prob 4-byte aligned.  Outputs overlap neither each other nor an input
- * (RR_ERR_INVALID_ARG).  Of cfg T, E and k are used.  Sums over tokens are held in 64 bits and added in a fixed order: results do not
+ * logits, rank_expert, loss, counts and mean_prob 4-byte aligned.  Outputs and workspace overlap neither each other nor an
+ * input (RR_ERR_INVALID_ARG).  Of cfg T, E and k are used.  Sums over tokens are held in 64 bits and added in a fixed order: results do not
  * change from run to run. */
 int rr_balance_workspace_bytes(const rr_config *cfg, size_t *bytes);
 int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *rank_expert, const uint8_t *token_mask,
@@ -278,7 +278,7 @@ int rr_linear_workspace_bytes(const rr_linear_config *cfg, int32_t backward, siz
 /*   x [M,K], w [R,K], bias [R] fp32 or NULL, residual [M,N] or NULL (may be y itself)
  *   y   [M,N] out
  *   pre [M,R] out or NULL: z, rounded to cfg->dtype, for rr_linear_backward
- * Outputs overlap neither each other nor an input (but y may be residual), or the call is refused (RR_ERR_INVALID_ARG).
+ * Outputs and workspace overlap neither each other nor an input (but y may be residual), or the call is refused (RR_ERR_INVALID_ARG).
  * Products are accumulated, and act and the sums made, in fp32; y is rounded once. */
 int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual,
               void *y, void *pre, void *workspace, size_t workspace_bytes, void *stream);
@@ -286,8 +286,8 @@ int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const f
 /* Gradients for dy [M,N]: with dz = dy act'(z) (bf16: rounded to bf16 for the two products)
  *     dx = dz W [M,K],   dw = dz^T x [R,K],   dbias = sum over rows of dz [R] fp32;   the residual's is dy.
  *   pre     the forward call's; ignored with RR_ACT_NONE
- *   dx, dw, dbias   each may be NULL (not all); x is needed for dw only and w for dx only, else NULL is allowed.  None of them may
- *                   overlap another or an input that is needed (RR_ERR_INVALID_ARG)
+ *   dx, dw, dbias   each may be NULL (not all); x is needed for dw only and w for dx only, else NULL is allowed.  None of them, nor the
+ *                   workspace, may overlap another or an input that is needed (RR_ERR_INVALID_ARG)
  * x, w, residual, y, pre, dy, dx and dw 16-byte aligned, bias and dbias 4-byte, the workspace 256-byte.  Sums run in a fixed
  * order: results do not change from run to run. */
 int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w, const void *pre, const void *dy,

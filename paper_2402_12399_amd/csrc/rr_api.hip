@@ -424,7 +424,7 @@ int rr_balance_loss(const rr_config *cfg, const float *logits, const int32_t *ra
     return RR_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < balance_workspace()) return RR_ERR_WORKSPACE;
   const size_t T = D.T, E = D.E;
-  if (any_meet({{loss, 4}, {counts, (E + 1) * 4}, {mean_prob, E * 4}}, {{logits, T * E * 4}, {rank_expert, T * (D.k + 1) * 4}, {token_mask, T}}))
+  if (any_meet({{loss, 4}, {counts, (E + 1) * 4}, {mean_prob, E * 4}, {workspace, balance_workspace()}}, {{logits, T * E * 4}, {rank_expert, T * (D.k + 1) * 4}, {token_mask, T}}))
     return RR_ERR_INVALID_ARG;
   const hipError_t e = launch_balance_loss(D.T, D.E, D.k, logits, rank_expert, token_mask, coef, loss, counts, mean_prob, workspace,
                                            static_cast<hipStream_t>(stream));
@@ -515,10 +515,10 @@ int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const f
   if (!x || !w || !y) return RR_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(w) || !aligned4(bias) || !aligned16(residual) || !aligned16(y) || !aligned16(pre))
     return RR_ERR_INVALID_ARG;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < linear_workspace(*cfg, false))
-    return RR_ERR_WORKSPACE;
+  const size_t need = linear_workspace(*cfg, false);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need) return RR_ERR_WORKSPACE;
   const LinearBytes L(*cfg);
-  if (any_meet({{y, L.y}, {pre, L.z}}, {{x, L.x}, {w, L.w}, {bias, L.bias}, {residual == y ? nullptr : residual, L.y}}))
+  if (any_meet({{y, L.y}, {pre, L.z}, {workspace, need}}, {{x, L.x}, {w, L.w}, {bias, L.bias}, {residual == y ? nullptr : residual, L.y}}))
     return RR_ERR_INVALID_ARG;
   if (device_setup() < 0) return RR_ERR_HIP;
   const hipError_t e = launch_linear(*cfg, x, w, bias, residual, y, pre, workspace, static_cast<hipStream_t>(stream));
@@ -532,10 +532,10 @@ int rr_linear_backward(const rr_linear_config *cfg, const void *x, const void *w
   if (!dy || (!dx && !dw && !dbias) || (dx && !w) || (dw && !x) || (cfg->act != RR_ACT_NONE && !pre)) return RR_ERR_INVALID_ARG;
   if (!aligned16(x) || !aligned16(w) || !aligned16(pre) || !aligned16(dy) || !aligned16(dx) || !aligned16(dw) || !aligned4(dbias))
     return RR_ERR_INVALID_ARG;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < linear_workspace(*cfg, true))
-    return RR_ERR_WORKSPACE;
+  const size_t need = linear_workspace(*cfg, true);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need) return RR_ERR_WORKSPACE;
   const LinearBytes L(*cfg);
-  if (any_meet({{dx, L.x}, {dw, L.w}, {dbias, L.bias}},
+  if (any_meet({{dx, L.x}, {dw, L.w}, {dbias, L.bias}, {workspace, need}},
                {{dy, L.y}, {dw ? x : nullptr, L.x}, {dx ? w : nullptr, L.w}, {cfg->act != RR_ACT_NONE ? pre : nullptr, L.z}}))
     return RR_ERR_INVALID_ARG;
   if (device_setup() < 0) return RR_ERR_HIP;

@@ -225,6 +225,38 @@ def test_balance_outputs_do_not_overlap(lib):
                 assert backward(flags, dlogits=place) == INVALID, (other, place)
 
 
+def test_workspaces_lie_apart(lib):
+    """What a call needs of its workspace shares no byte with an operand; what lies behind that may."""
+    ends = lambda start, size, need: (start - need + 256, start, start + (size - 1) // 256 * 256)
+    M, K, N, gap = 16, 64, 32, 1 << 22
+    c = _linear(M=M, K=K, N=N, act=rr.RR_ACT_SWIGLU)
+    x, w, y, z, b = M * K * 2, 2 * N * K * 2, M * N * 2, M * 2 * N * 2, 2 * N * 4
+    need = C.c_size_t(0)
+    size = dict(x=x, w=w, bias=b, residual=y, y=y, pre=z)
+    good = {name: gap * (i + 1) for i, name in enumerate(size)}
+    a = {name: at(v) for name, v in good.items()}
+    assert lib.rr_linear_workspace_bytes(C.byref(c), 0, C.byref(need)) == 0 and need.value < gap
+    for name in size:
+        for place in ends(good[name], size[name], need.value):
+            assert lib.rr_linear(C.byref(c), a["x"], a["w"], a["bias"], a["residual"], a["y"], a["pre"], at(place), BIG, None) == INVALID, (name, place)
+    size = dict(x=x, w=w, pre=z, dy=y, dx=x, dw=w, dbias=b)
+    good = {name: gap * (i + 1) for i, name in enumerate(size)}
+    a = {name: at(v) for name, v in good.items()}
+    assert lib.rr_linear_workspace_bytes(C.byref(c), 1, C.byref(need)) == 0 and need.value < gap
+    for name in size:
+        for place in ends(good[name], size[name], need.value):
+            assert lib.rr_linear_backward(C.byref(c), a["x"], a["w"], a["pre"], a["dy"], a["dx"], a["dw"], a["dbias"], at(place), BIG, None) == INVALID, (name, place)
+    T, E, k = 64, 8, 2
+    c = rr.RRConfig(T=T, d_model=64, d_ff=0, E=E, k=k, G=2, capacity_factor=1.0).c()
+    size = dict(logits=4 * T * E, rank=4 * T * (k + 1), mask=T, loss=4, counts=4 * (E + 1), mean=4 * E)
+    good = {name: gap * (i + 1) for i, name in enumerate(size)}
+    a = {name: at(v) for name, v in good.items()}
+    assert lib.rr_balance_workspace_bytes(C.byref(c), C.byref(need)) == 0 and need.value < gap
+    for name in size:
+        for place in ends(good[name], size[name], need.value):
+            assert lib.rr_balance_loss(C.byref(c), a["logits"], a["rank"], a["mask"], 0.1, a["loss"], a["counts"], a["mean"], at(place), BIG, None) == INVALID, (name, place)
+
+
 def test_dropout_refusals(lib):
     def call(n=64, dtype=rr.RR_BF16, x=FAKE, residual=None, p=0.1, dev=None, out=FAKE):
         a = lib.rr_dropout(n, dtype, x, residual, p, 1, 2, dev, out, None)
