@@ -248,7 +248,7 @@ int rr_balance_loss_backward(const rr_config *cfg, const float *logits, const in
  *   p              0 <= p <= 1, taken in steps of 1 / 65536; at p = 1 out is the residual (or 0)
  *   device_offset  NULL, or one uint64 on the device (8-byte aligned) that is added to `offset` when the kernel runs: a captured
  *                  graph then draws another mask in each replay
- *   out            [n]; may be x or residual itself, but not overlap one of them otherwise (RR_ERR_INVALID_ARG)
+ *   out            [n]; may be x or residual itself, but not overlap one of them otherwise, nor device_offset (RR_ERR_INVALID_ARG)
  * A dropped element leaves nothing behind, whatever its value (NaN and infinities too).  The sum is made in fp32 and rounded
  * once.  All data pointers 16-byte aligned. */
 int rr_dropout(int64_t n, int32_t dtype, const void *x, const void *residual, float p, uint64_t seed, uint64_t offset,

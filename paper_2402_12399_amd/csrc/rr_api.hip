@@ -455,6 +455,7 @@ static int dropout(int64_t n, int32_t dtype, const void *x, const void *residual
   const size_t bytes = (size_t)n * (dtype == RR_BF16 ? 2 : 4);
   for (const void *in : {x, residual})
     if (in != out && meet({in, bytes}, {out, bytes})) return RR_ERR_INVALID_ARG;
+  if (meet({device_offset, 8}, {out, bytes})) return RR_ERR_INVALID_ARG;
   const u32 m = (u32)floor(65536.0 * (double)p + 0.5);
   const hipError_t e = launch_dropout(n, dtype, x, residual, m, seed, offset, reinterpret_cast<const unsigned long long *>(device_offset),
                                       out, id, static_cast<hipStream_t>(stream));

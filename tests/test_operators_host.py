@@ -257,6 +257,15 @@ def test_workspaces_lie_apart(lib):
             assert lib.rr_balance_loss(C.byref(c), a["logits"], a["rank"], a["mask"], 0.1, a["loss"], a["counts"], a["mean"], at(place), BIG, None) == INVALID, (name, place)
 
 
+def test_dropout_counter_outside_the_result(lib):
+    """device_offset is read by every workgroup, some after others have written."""
+    gap, n = 1 << 15, 1000
+    for place in (0, 8, 2 * n - 8):
+        assert lib.rr_dropout(n, rr.RR_BF16, at(0), None, 0.1, 1, 2, at(gap + place), at(gap), None) == INVALID
+        assert lib.rr_dropout(n, rr.RR_BF16, at(0), at(gap), 0.1, 1, 2, at(gap + place), at(gap), None) == INVALID
+        assert lib.rr_dropout_backward(n, rr.RR_BF16, at(gap), 0.1, 1, 2, at(gap + place), at(gap), None) == INVALID
+
+
 def test_dropout_refusals(lib):
     def call(n=64, dtype=rr.RR_BF16, x=FAKE, residual=None, p=0.1, dev=None, out=FAKE):
         a = lib.rr_dropout(n, dtype, x, residual, p, 1, 2, dev, out, None)
