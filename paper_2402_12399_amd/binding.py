@@ -365,19 +365,19 @@ def _dropout_type(what: str, t):
     return dtype, RR_F32 if dtype is _torch().float32 else RR_BF16
 
 
-def _no_wrap64(what: str, seed: int, offset: int):
+def _check_seed(what: str, seed: int):
     """Refuses what the C call would cut to 64 bits.  (A negative number that fits is the unsigned one of the same bits.)"""
-    if not (-1 << 63 <= seed < 1 << 64 and -1 << 63 <= offset < 1 << 64):
-        raise RRError(f"{what}: seed {seed} or offset {offset} does not fit in 64 bits")
+    if not -1 << 63 <= seed < 1 << 64:
+        raise RRError(f"{what}: seed {seed} does not fit in 64 bits")
 
 
 def rr_dropout(x, p: float, seed: int, offset: int, out, residual=None, device_offset=None):
     """out = residual + dropout(x), any shape; out may be x or residual.  device_offset: None or one int64 on the GPU, added to
-    `offset` when the kernel runs (captured graphs).  A call uses up (x.numel() + 7) // 8 counters from `offset` on.  seed and offset are
-    numbers of 64 bits; others are refused."""
+    `offset` when the kernel runs (captured graphs).  A call uses up (x.numel() + 7) // 8 counters from `offset` on.  A seed has
+    64 bits, or is refused; counters, and `offset` with them, are taken modulo 2^64."""
     me, n = "rr_dropout", x.numel()
     t, dtype = _dropout_type(me, x)
-    _no_wrap64(me, seed, offset)
+    _check_seed(me, seed)
     d = _device(me, x)
     _check(load_library().rr_dropout(
         n, dtype, _addr(me, "x", x, n, t, d), _addr(me, "residual", residual, n, t, d), p, seed, offset,
@@ -388,7 +388,7 @@ def rr_dropout_backward(dout, p: float, seed: int, offset: int, dx, device_offse
     """dx from dout with the mask of the forward call of the same p, seed and offset; dx may be dout."""
     me, n = "rr_dropout_backward", dout.numel()
     t, dtype = _dropout_type(me, dout)
-    _no_wrap64(me, seed, offset)
+    _check_seed(me, seed)
     d = _device(me, dout)
     _check(load_library().rr_dropout_backward(
         n, dtype, _addr(me, "dout", dout, n, t, d), p, seed, offset,
