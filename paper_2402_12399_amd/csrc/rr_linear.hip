@@ -240,15 +240,17 @@ __global__ __launch_bounds__(256) void linear_join_kernel(DenseArgs P) {
 
 // ------------------------------------------------------------------ dz, transposes, column sums
 // A workgroup takes 64 columns of dy (or of x, or W: ACT none), 64 rows at a time (every gridDim.y-th tile of them), makes dz where there
-// is an activation, and writes what is asked for: dz, its transpose of row pitch LT >= M (zeros behind column M), the sums of its
-// columns over all its rows.  A thread owns two neighbouring rows and eight columns, so that the transpose goes through LDS in words.
+// is an activation, and writes what is asked for: dz, the sums of its columns over all its rows, and (fp32; bf16 products read every
+// operand as it lies) its transpose of row pitch LT >= M, zeros behind column M, through LDS.  A thread owns two neighbouring rows and eight
+// columns.
 // bf16: dz is rounded once before the products, whose matrix instructions read bf16; the column sums take it unrounded.  The gradients are then two
 // roundings off, 2.3e-3 in norm, where the exact ones rounded once are 1.7e-3.  As two bf16 parts dz would double both summations: 8192 rows, 2048 ->
 // 2 x 5632, the products 581 us, 1146 with twice the columns of dz.
 // Bound by HBM: 8192 x 5632 bf16 SwiGLU, dz alone: 89 us, 461 MB, 5.2 TB/s.
 struct TurnArgs {
   const void *src, *pre;  // [M, N], [M, R]
-  void *dz, *turned;      // [M, R], [R, LT]
+  void *dz;               // [M, R]
+  float *turned;          // [R, LT]
   float *sums;            // [gridDim.y, R]
   int M, N, LT;
 };
@@ -309,11 +311,9 @@ __device__ inline float gelu_slope(float z) {
 template <bool BF16, int ACT>
 __global__ __launch_bounds__(TN_THREADS) void linear_turn_kernel(TurnArgs P) {
   constexpr int NB = ACT == RR_ACT_SWIGLU ? 2 : 1;
-  constexpr int PITCH = BF16 ? TN_TILE / 2 + 1 : TN_TILE + 1;  // words of a column in LDS: odd, so that no two lanes meet in a bank
-  __shared__ u32 tile[TN_TILE * PITCH];
   __shared__ float part[TN_THREADS / kWave][TN_TILE];
   const int tid = threadIdx.x, piece = tid & 7, pair = tid >> 3, N = P.N, R = NB * N;
-  const int n0 = blockIdx.x * TN_TILE, col = n0 + piece * 8, rows = P.turned ? max(P.M, P.LT) : P.M;
+  const int n0 = blockIdx.x * TN_TILE, col = n0 + piece * 8, rows = !BF16 && P.turned ? max(P.M, P.LT) : P.M;
   float sum[NB][8];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
@@ -354,28 +354,26 @@ __global__ __launch_bounds__(TN_THREADS) void linear_turn_kernel(TurnArgs P) {
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[b][i] += v[b][0][i] + v[b][1][i];
-      if (!P.turned) continue;
-      __syncthreads();  // the tile before this one has been read
+      if constexpr (!BF16) {
+        if (!P.turned) continue;
+        constexpr int PITCH = TN_TILE + 1, PIECES = TN_TILE / 4;  // words of a column in LDS: odd, so that no two lanes meet in a bank; 16-byte pieces
+        __shared__ float tile[TN_TILE * PITCH];
+        __syncthreads();  // the tile before this one has been read
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        u32 *at = tile + (piece * 8 + i) * PITCH;
-        if constexpr (BF16) {
-          at[pair] = pack_bf16(v[b][0][i], v[b][1][i]);
-        } else {
-          at[2 * pair] = __builtin_bit_cast(u32, v[b][0][i]);
-          at[2 * pair + 1] = __builtin_bit_cast(u32, v[b][1][i]);
+        for (int i = 0; i < 8; ++i) {
+          float *at = tile + (piece * 8 + i) * PITCH + 2 * pair;
+          at[0] = v[b][0][i];
+          at[1] = v[b][1][i];
         }
-      }
-      __syncthreads();
-      constexpr int WORDS = BF16 ? TN_TILE / 2 : TN_TILE, PIECES = WORDS / 4;  // of a turned row; 16-byte pieces
+        __syncthreads();
 #pragma unroll
-      for (int k = 0; k < TN_TILE * PIECES / TN_THREADS; ++k) {
-        const int p = k * TN_THREADS + tid, c = p / PIECES, q = p % PIECES;
-        const u32 *at = tile + c * PITCH + q * 4;
-        const int m = m0 + q * (BF16 ? 8 : 4);
-        if (n0 + c < N && m < P.LT)
-          *reinterpret_cast<uint4 *>(static_cast<char *>(P.turned) + ((size_t)(b * N + n0 + c) * P.LT + m) * (BF16 ? 2 : 4)) =
-              make_uint4(at[0], at[1], at[2], at[3]);
+        for (int k = 0; k < TN_TILE * PIECES / TN_THREADS; ++k) {
+          const int p = k * TN_THREADS + tid, c = p / PIECES, q = p % PIECES;
+          const float *at = tile + c * PITCH + q * 4;
+          const int m = m0 + q * 4;
+          if (n0 + c < N && m < P.LT)
+            *reinterpret_cast<float4 *>(P.turned + (size_t)(b * N + n0 + c) * P.LT + m) = make_float4(at[0], at[1], at[2], at[3]);
+        }
       }
     }
   }
@@ -650,7 +648,8 @@ void launch_turn(int act, const TurnArgs &A, hipStream_t s) {
 
 // Workspace of the backward pass.
 struct BackwardWork {
-  void *dz, *dz_turned, *x_turned, *w_turned;
+  void *dz;
+  float *dz_turned, *x_turned, *w_turned;  // fp32 only
   float *sums, *part;
   int LT;  // row pitch of the transposes that are summed over rows: M and zeros up to whole chunks
   size_t bytes;
@@ -664,14 +663,15 @@ BackwardWork backward_work(const rr_linear_config &c, void *ws) {
     off += up256(n);
     return p;
   };
+  auto take_floats = [&](size_t n) { return static_cast<float *>(take(n * 4)); };
   const size_t R = width(c), es = element(c);
   W.LT = (c.M + 63) / 64 * 64;
   W.dz = take(c.act == RR_ACT_NONE ? 0 : (size_t)c.M * R * es);
   const bool turns = c.dtype != RR_BF16;
-  W.dz_turned = take(turns ? R * W.LT * es : 0);
-  W.x_turned = take(turns ? (size_t)c.K * W.LT * es : 0);
-  W.w_turned = take(turns ? (size_t)c.K * R * es : 0);
-  W.sums = static_cast<float *>(take((size_t)(W.LT / TN_TILE) * R * 4));
+  W.dz_turned = take_floats(turns ? R * W.LT : 0);
+  W.x_turned = take_floats(turns ? (size_t)c.K * W.LT : 0);
+  W.w_turned = take_floats(turns ? (size_t)c.K * R : 0);
+  W.sums = take_floats((size_t)(W.LT / TN_TILE) * R);
   W.part = static_cast<float *>(take(std::max(part_reserve(c.M, c.K), part_reserve(R, c.K))));
   W.bytes = off;
   return W;
