@@ -397,6 +397,53 @@ def test_the_gpu_tests_reach_every_tile(lib):
             assert set(_plan_keys(M, K, N)) <= reached, (M, K, N, set(_plan_keys(M, K, N)) - reached)
 
 
+def _kernel_keys(M, K, N, dtype, act, roles=(0, 1, 2)):
+    """One key per kernel that the products of a call are made by: the activation is a part of the forward one's."""
+    from tests import gpu_util as gu
+    cfg = rr.RRLinearConfig(M, K, N, dtype, act)
+    for role, (bm, brows, slices, parts) in enumerate(gu.linear_plans(cfg)):
+        if role not in roles:
+            continue
+        few = 0
+        if bm == 0:  # one kernel per number of rows up to the dot products' most, then one up to 16 and one up to 32
+            rows = cfg.rows if role == 2 else M
+            few = rows if rows <= (2 if dtype == rr.RR_BF16 else 4) else 16 if rows <= 16 else 32
+        once = role == 0 and dtype == rr.RR_BF16 and 0 < M <= bm and (bm, brows) != (256, 256)  # (weights read once)
+        yield dtype, act if role == 0 else None, role, bm, brows, parts, slices > 1, once, few
+
+
+def test_the_gpu_tests_run_every_kernel(lib):
+    """Whatever kernels the plan gives products of up to 6e10 multiplications, one of the GPU tests runs them and compares: counted from what each
+    of those tests calls, with its types and activations."""
+    from tests import test_gpu_operators as t, test_gpu_operators_tiles as tiles
+    none, gelu, swiglu = rr.RR_ACT_NONE, rr.RR_ACT_GELU, rr.RR_ACT_SWIGLU
+    both = (rr.RR_F32, rr.RR_BF16)
+    runs = [(s, d, none, (0, 1, 2)) for s in t.SHAPES + t.MORE for d in both]  # test_linear_exact_sums
+    runs += [(s, d, swiglu, (0,)) for s in t.MORE for d in both]  # test_linear_gated_tiles
+    runs += [(s, d, a, (0, 1, 2)) for s in t.SHAPES for d in both for a in (gelu, swiglu)]  # test_linear_values_and_gradients
+    runs += [(l[:3], rr.RR_BF16, none, (0, 1, 2) if l[3] == "none" else (1, 2)) for l in t.LARGE]  # test_linear_large_tiles
+    runs += [(f[2:5], rr.RR_F32 if f[0] == "f32" else rr.RR_BF16, t.ACT[f[1]], (0,)) for f in tiles.FORWARD]
+    runs += [(g[1:4], rr.RR_F32 if g[0] == "f32" else rr.RR_BF16, none, (tiles.ROLE[g[4]],)) for g in tiles.GRADIENTS]
+    reached = {k for s, d, a, roles in runs for k in _kernel_keys(*s, d, a, roles)}
+    rng = np.random.default_rng(8)
+    for _ in range(6000):
+        M, K, N = int(2 ** rng.uniform(0, 16)), 8 * int(2 ** rng.uniform(0, 11)), 8 * int(2 ** rng.uniform(0, 11))
+        if M * K * N <= 6e10 and M * max(K, N) <= 1e8:
+            for d in both:
+                for a in (none, gelu, swiglu):
+                    keys = set(_kernel_keys(M, K, N, d, a))
+                    assert keys <= reached, (M, K, N, keys - reached)
+
+
+def test_the_gpu_tests_tiles_are_the_plan_s(lib):
+    """Each case of test_gpu_operators_tiles.py is about the kernel that it names."""
+    from tests import test_gpu_operators_tiles as tiles
+    for dtype, act, M, K, N, *plan in tiles.FORWARD:
+        tiles.assert_plan(tiles.config(dtype, act, M, K, N), 0, *plan)
+    for dtype, M, K, N, name, *plan in tiles.GRADIENTS:
+        tiles.assert_plan(tiles.config(dtype, "none", M, K, N), tiles.ROLE[name], *plan)
+
+
 def test_linear_slices_fit_the_workspace(lib):
     """The slices' sums, rows x columns x slices floats, fit what the workspace keeps for them, and no slice is empty."""
     from tests import gpu_util as gu
