@@ -1,5 +1,6 @@
 """GPU tests of the dense projection's kernels: every tile of the forward product with every activation, with and without slices of the
-summation, and the gradients' tiles that other shapes leave out.  Each test first says which tiles it is about, so that a change of the plan cannot move it elsewhere unseen
+summation, the gradients' tiles that other shapes leave out, and numbers that are not finite next to the edges of the largest
+tiles.  Each test first says which tiles it is about, so that a change of the plan cannot move it elsewhere unseen
 (test_operators_host.py checks that the shapes leave none out).  Whole numbers, as in test_gpu_operators.py: sums are exact."""
 import pytest
 import torch
@@ -7,7 +8,7 @@ import torch
 import paper_2402_12399_amd as rr
 from tests import gpu_util as gu
 from tests import operators_ref as ref
-from tests.test_gpu_operators import ACT, DT, F32, U, V, gen, linear_case, nearest, run_backward, run_linear, whole, within
+from tests.test_gpu_operators import ACT, BF16, DT, F32, U, V, Guarded, gen, linear_case, nearest, run_backward, run_linear, whole, within
 
 pytestmark = pytest.mark.gpu
 
@@ -88,3 +89,55 @@ def test_gradient_tiles(dtype, M, K, N, name, tile, several, parts):
     got = run_backward(x, w, None, dy, "none", dtype, N)
     for n in got:
         assert torch.equal(got[n], nearest(want[n], dtype) if n != "dbias" else want[n].to(F32)), n
+
+
+def between_nan(t):
+    """A copy that lies between NaN: what a kernel reads before or behind an operand shows in its sums."""
+    g = Guarded(tuple(t.shape), t.dtype)
+    g.t.copy_(t)
+    return g.t
+
+
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("M,K,N", [(4099, 1000, 4104), (2051, 4160, 4104)])
+def test_not_finite_in_large_forward_tiles(M, K, N, act):
+    """x[m, k] reaches row m of y, w[n, k] column n - also from the first elements of a row, which follow the last ones of the row before in memory."""
+    assert_plan(config("bf16", act, M, K, N), 0, (256, 256), False, False)
+    x, w, _, _, _ = linear_case(M, K, N, "bf16", "none", whole, 17, False, False)
+    x, w = between_nan(x), between_nan(w)
+    _, clean = run_linear(x, w, None, None, act, "bf16", N)
+    assert bool(torch.isfinite(clean).all())
+    nan, inf = float("nan"), float("inf")
+    x[5, 3], x[8, 0], x[300, K - 1], x[M - 1, 1] = nan, inf, -inf, nan
+    w[11, 2], w[260, 0], w[N - 1, K - 1] = inf, nan, nan
+    cfg, y, z = config("bf16", act, M, K, N), torch.empty_like(clean), torch.empty_like(clean)
+    rr.rr_linear(cfg, x, w, None, None, y, z, rr.alloc_linear_workspace(cfg))
+    rows, cols = torch.ones(M, dtype=torch.bool, device="cuda"), torch.ones(N, dtype=torch.bool, device="cuda")
+    rows[[5, 8, 300, M - 1]] = False
+    cols[[11, 260, N - 1]] = False
+    assert torch.equal(z[rows][:, cols], clean[rows][:, cols]) and bool(torch.isfinite(y[rows][:, cols]).all())
+    assert not bool(torch.isfinite(z[~rows]).any()) and not bool(torch.isfinite(z[:, ~cols]).any())
+
+
+@pytest.mark.parametrize("M,K,N", [(8195, 2048, 1416), (2051, 4160, 4104)])
+def test_not_finite_in_large_turned_tiles(M, K, N):
+    """x[m, k] reaches column k of dw, dy[m, n] row m of dx and row n of dw, w[n, k] column k of dx.  Both summations end inside a
+    chunk, whose other rows and pieces read as zero, and the staged rows of ragged tiles go on into the next row of the memory."""
+    plans = gu.linear_plans(config("bf16", "none", M, K, N))
+    assert plans[1][:2] == (256, 256) and plans[2][:2] == (256, 256) and N % 64 and M % 64
+    x, w, _, _, _ = linear_case(M, K, N, "bf16", "none", whole, 18, False, False)
+    x, w, dy = between_nan(x), between_nan(w), between_nan(whole(gen(19), M, N, dtype=BF16))
+    clean = run_backward(x, w, None, dy, "none", "bf16", N, ("dx", "dw"))
+    want = ref.linear_backward(x, w, None, dy, "none")
+    assert all(torch.equal(clean[n], nearest(want[n], "bf16")) for n in clean)
+    nan, inf = float("nan"), float("inf")
+    x[5, 3], x[M - 1, 0], x[100, K - 1] = nan, inf, nan
+    dy[7, 2], dy[9, 0], dy[M - 1, 1], dy[50, N - 1] = inf, nan, nan, -inf
+    w[11, 0], w[N - 1, 5] = inf, nan
+    cfg, dx, dw = config("bf16", "none", M, K, N), torch.empty_like(x), torch.empty_like(w)
+    rr.rr_linear_backward(cfg, x, w, None, dy, dx, dw, None, rr.alloc_linear_workspace(cfg, True))
+    keep = lambda n, gone: torch.tensor([i not in gone for i in range(n)], device="cuda")
+    for got, ok, rows, cols in ((dx, clean["dx"], keep(M, (7, 9, M - 1, 50)), keep(K, (0, 5))),
+                                (dw, clean["dw"], keep(N, (0, 1, 2, N - 1)), keep(K, (0, 3, K - 1)))):
+        assert torch.equal(got[rows][:, cols], ok[rows][:, cols])
+        assert not bool(torch.isfinite(got[~rows]).any()) and not bool(torch.isfinite(got[:, ~cols]).any())
