@@ -240,7 +240,8 @@ __global__ __launch_bounds__(BG_THREADS) void balance_grad_kernel(BalanceGradArg
   const int lane = threadIdx.x & (kWave - 1), w = threadIdx.x >> 6, E = A.E;
   const int n = A.counts[E];
   const float each = n > 0 ? 1.0f / ((float)A.k * (float)n) : 0.0f;
-  const float scale = n > 0 ? (A.dloss ? *A.dloss : 1.0f) * A.coef * (float)E / (float)n : 0.0f;
+  // (in 64 bits: dloss coef and coef E may lie outside fp32's range where the quotient does not)
+  const float scale = n > 0 ? (float)((double)(A.dloss ? *A.dloss : 1.0f) * A.coef * E / n) : 0.0f;
   // f_e less the mean of all: the mean falls out of f_e - sum_j f_j p_tj, as the p_tj add up to 1, and with it goes most of what would
   // cancel where the experts are nearly balanced (all alike: zeros, not rounding errors).  Differences of whole numbers are exact.
   int32_t count[4], sum = 0;

@@ -237,6 +237,14 @@ def test_balance_edges():
         assert not bool(grad.any())
 
 
+@pytest.mark.parametrize("coef,dloss", [(1e37, 1.0), (-1e37, 1.5), (1e30, 1e8), (1e-37, 1e30), (1e-30, 1e-12)])
+def test_balance_of_any_finite_coefficient(coef, dloss):
+    """coef times the experts and dloss times coef may lie outside fp32's range; their quotient by the tokens does not."""
+    g, T, E = gen(15), 300, 64
+    a = normal(g, T, E)
+    check_balance(a, ranks_of(a, 2), 2, coef, None, dloss)
+
+
 @pytest.mark.parametrize("E", [6, 7, 8, 64])
 def test_balance_accumulates_and_takes_any_alignment(E):
     g, T = gen(6), 333
