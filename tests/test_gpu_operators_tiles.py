@@ -80,6 +80,16 @@ def test_forward_tiles(dtype, act, M, K, N, tile, several, parts):
         within(y, want, e + (V if dtype == "bf16" else U) * (want.abs() + e) + 1e-38, "y")
 
 
+@pytest.mark.parametrize("dtype,act,M,K,N,tile,several,parts", [f for f in FORWARD if f[5] >= (128, 128)])
+def test_forward_tiles_in_place(dtype, act, M, K, N, tile, several, parts):
+    """y may be the residual: lanes trade columns of it before they store."""
+    x, w, b, r, _ = linear_case(M, K, N, dtype, act, whole, M + N)
+    y, _ = run_linear(x, w, b, r, act, dtype, N)
+    cfg = config(dtype, act, M, K, N)
+    rr.rr_linear(cfg, x, w, b, r, r, None, rr.alloc_linear_workspace(cfg))
+    assert torch.equal(y, r)
+
+
 @pytest.mark.parametrize("dtype,M,K,N,name,tile,several,parts", GRADIENTS)
 def test_gradient_tiles(dtype, M, K, N, name, tile, several, parts):
     assert_plan(config(dtype, "none", M, K, N), ROLE[name], tile, several, parts)
