@@ -119,7 +119,7 @@ typedef struct rr_tables {
 
 /* One-time, per-device host-side set-up for the current device: raises the dynamic-LDS limit of the
  * grouped-GEMM kernels and looks up the address of the static scratch buffer.  Idempotent and
- * thread-safe.  Every entry point runs it on its first call on a device; call it explicitly before
+ * thread-safe.  Every entry point that needs any of it runs it on its first call on a device; call it explicitly before
  * capturing calls in a HIP graph.  Returns RR_OK or RR_ERR_HIP. */
 int rr_init(void);
 

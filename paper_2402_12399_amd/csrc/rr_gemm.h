@@ -1120,7 +1120,7 @@ __global__ __launch_bounds__(S::THREADS, S::OCC) void gemm_tile_kernel(typename 
     auto fetch_turned = [&](f32x4 *r, int n, const __amdgpu_buffer_rsrc_t &rs, int k, int c, unsigned pitch) {
       unsigned at = k * n * pitch + c * 16;
       // Tiles of 64 rows add up the other offsets again for every chunk: kept in registers, they make others spill (20000 x 512 -> 512
-      // 169 us, 159 so; 128 x 128 tiles lose 2 % by it)
+      // 169 us, 159 so; 128 x 128 tiles, which spill two or three, lose 2 % by it)
       if (WM == 2) asm volatile("" : "+v"(at));
 #pragma unroll
       for (int i = 0; i < n; ++i) r[i] = load16(rs, at + i * pitch, 0);

@@ -719,7 +719,7 @@ void linear_describe(const rr_linear_config &c, LinearPlans *out) {
     out->bm[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].bm;
     out->brows[i] = plan[i].shape < 0 ? 0 : kShape[plan[i].shape].brows;
     out->slices[i] = plan[i].slices;
-    out->parts[i] = plan[i].shape == FFN_S128 || plan[i].shape == FFN_S64;
+    out->parts[i] = splits(plan[i]);
   }
 }
 
