@@ -9,7 +9,8 @@
 // again rather than stored.
 // Bound by HBM and, a little below it, by the instructions of exponentials and reductions.  2^20 tokens, 64 experts, top-2: loss
 // 55 us + 6 (281 MB, 4.6 TB/s; with expf, shuffles through LDS, a lane per row for the choices and one row at a time 135 + 30),
-// gradient 86 us (537 MB, 6.2 TB/s).  1001 tokens, 16 experts: 6.4 and 3.6 us, one workgroup without records.
+// gradient 84 us (537 MB, 6.4 TB/s), added to what is there 153 (805 MB, 5.3 TB/s).  1001 tokens, 16 experts: 6.4 and 3.8 us, one workgroup
+// without records.
 #include "rr_device.h"
 
 namespace rr {
