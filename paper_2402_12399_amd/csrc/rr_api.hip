@@ -509,6 +509,13 @@ int rr_linear_plans(const rr_linear_config *cfg, LinearPlans *out) {
   return rc;
 }
 
+// Host function for tests: see linear_cut.
+int rr_linear_cut(int32_t m0, int32_t rows, int32_t cut, int32_t part, int32_t *range) {
+  if (!range || m0 < 0 || rows <= 0 || cut <= 0 || part < 0 || part >= cut) return RR_ERR_INVALID_ARG;
+  linear_cut(m0, rows, cut, part, range);
+  return RR_OK;
+}
+
 int rr_linear(const rr_linear_config *cfg, const void *x, const void *w, const float *bias, const void *residual, void *y, void *pre,
               void *workspace, size_t workspace_bytes, void *stream) {
   const int rc = check_linear(cfg);

@@ -329,6 +329,15 @@ constexpr int PK_SMEM = PK_B_BASE + PK_B_STAGES * PK_B_STAGE;  // 160 KB: all of
 [[maybe_unused]] constexpr int PK_NI = (PK_BM + PK_BROWS) / 8 / PK_NW;  // 1 KB load instructions per wave per chunk
 [[maybe_unused]] constexpr int PK_NIA = PK_BM / 8 / PK_NW;
 
+// Part `part` of a tile of `rows` rows from m0 on that is cut into `cut`: an equal share in whole fragments of both waves, which may leave
+// the last parts short or empty (m0 >= end).  No part passes the tile's end: a row computed twice adds its residual twice where y
+// lies in the residual's place.
+struct CutRows { int m0, end; };
+__host__ __device__ inline CutRows cut_rows(int m0, int rows, int cut, int part) {
+  const int h = (rows + cut * 32 - 1) / (cut * 32) * 32, a = part * h, b = a + h;
+  return {m0 + a, m0 + (b < rows ? b : rows)};
+}
+
 // Turned operands (TA, TB; dense products, bf16): the summation runs down the memory's rows, as in dx = dz W and dw = dz^T x.  A
 // chunk is then 64 memory rows of as many neighbouring columns as the tile has rows, staged as they lie (a DMA instruction fills
 // 1 KB of them), and the fragments come out of LDS through ds_read_b64_tr_b16: 16 lanes name the 4 pieces of 8 bytes of each of
@@ -509,10 +518,10 @@ __global__ __launch_bounds__(PK_THREADS) void gemm_bf16_persistent_kernel(typena
       f.rbase = f.fill_e = f.iroff_e = 0;
       f.rows_e = P.M;
     }
-    if (u.part >= 0) {  // an equal share of the tile's rows, in whole fragments of both waves; past the last row: empty
-      const int h = (min(BM, f.rows_e - f.m0) + cut * 32 - 1) / (cut * 32) * 32;
-      f.m0 += u.part * h;
-      f.rows_e = min(f.rows_e, f.m0 + h);
+    if (u.part >= 0) {
+      const CutRows r = cut_rows(f.m0, min(BM, f.rows_e - f.m0), cut, u.part);
+      f.m0 = r.m0;
+      f.rows_e = r.end;
     }
     return f;
   };

@@ -176,6 +176,8 @@ hipError_t linear_kernel_attributes();  // as ffn_kernel_attributes
 // parts: for tests (rr_linear_plans, exported by the library but no part of its C ABI).
 struct LinearPlans { int32_t bm[3], brows[3], slices[3], parts[3]; };
 void linear_describe(const rr_linear_config &c, LinearPlans *out);
+// First row and end of a part of a 256 x 256 kernel's tile of `rows` rows that is cut into `cut` parts: for tests too (rr_linear_cut).
+void linear_cut(int m0, int rows, int cut, int part, int32_t *range);
 size_t linear_workspace(const rr_linear_config &c, bool backward);
 hipError_t launch_linear(const rr_linear_config &c, const void *x, const void *w, const float *bias, const void *residual, void *y,
                          void *pre, void *ws, hipStream_t s);

@@ -723,6 +723,12 @@ void linear_describe(const rr_linear_config &c, LinearPlans *out) {
   }
 }
 
+void linear_cut(int m0, int rows, int cut, int part, int32_t *range) {
+  const CutRows r = cut_rows(m0, rows, cut, part);
+  range[0] = r.m0;
+  range[1] = r.end;
+}
+
 size_t linear_workspace(const rr_linear_config &c, bool backward) {
   return backward ? backward_work(c, nullptr).bytes : std::max<size_t>(256, part_reserve(c.M, width(c)));
 }

@@ -90,6 +90,25 @@ def test_forward_tiles_in_place(dtype, act, M, K, N, tile, several, parts):
     assert torch.equal(y, r)
 
 
+@pytest.mark.parametrize("act,M,K,N,cut", [("swiglu", 2057, 456, 4488, 3), ("swiglu", 2314, 456, 3720, 5), ("swiglu", 2057, 456, 4104, 6), ("swiglu", 2314, 456, 3592, 7),
+                                           ("none", 5655, 456, 3336, 3), ("none", 7454, 456, 2312, 5), ("gelu", 8225, 456, 2056, 6), ("none", 7197, 456, 2312, 7)])
+def test_cut_tiles_add_the_residual_once(act, M, K, N, cut):
+    """Tiles of the last round, cut by rows into parts whose equal shares do not add up to the tile: no row is computed twice, which y in the residual's
+    place would show."""
+    assert_plan(config("bf16", act, M, K, N), 0, (256, 256), False, False)
+    columns = 128 if act == "swiglu" else 256
+    left = -(-M // 256) * -(-N // columns) % torch.cuda.get_device_properties(0).multi_processor_count
+    assert torch.cuda.get_device_properties(0).multi_processor_count // left == cut
+    x, w, b, r, _ = linear_case(M, K, N, "bf16", act, whole, M + N)
+    y, _ = run_linear(x, w, b, r, act, "bf16", N, pre=False)
+    cfg = config("bf16", act, M, K, N)
+    ws = rr.alloc_linear_workspace(cfg)
+    for i in range(20):
+        at = r.clone()
+        rr.rr_linear(cfg, x, w, b, at, at, None, ws)
+        assert torch.equal(y, at), i
+
+
 @pytest.mark.parametrize("dtype,M,K,N,name,tile,several,parts", GRADIENTS)
 def test_gradient_tiles(dtype, M, K, N, name, tile, several, parts):
     assert_plan(config(dtype, "none", M, K, N), ROLE[name], tile, several, parts)

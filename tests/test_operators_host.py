@@ -444,6 +444,20 @@ def test_the_gpu_tests_tiles_are_the_plan_s(lib):
         tiles.assert_plan(tiles.config(dtype, "none", M, K, N), tiles.ROLE[name], *plan)
 
 
+@pytest.mark.parametrize("cut", range(1, 9))
+def test_parts_of_a_cut_tile_share_no_row(lib, cut):
+    """The last round of 256 x 256 tiles is cut by rows into up to eight parts: together they are the tile, no row twice (y may lie in the
+    residual's place) and none of the next tile's."""
+    for m0 in (0, 256, 3840):
+        for rows in range(1, 257):
+            got = []
+            for part in range(cut):
+                r = (C.c_int32 * 2)()
+                assert lib.rr_linear_cut(m0, rows, cut, part, r) == 0
+                got += range(r[0], r[1])
+            assert got == list(range(m0, m0 + rows)), (m0, rows, cut)
+
+
 def test_linear_slices_fit_the_workspace(lib):
     """The slices' sums, rows x columns x slices floats, fit what the workspace keeps for them, and no slice is empty."""
     from tests import gpu_util as gu
